@@ -14,6 +14,10 @@
  *                                          the attention stage for training and its backward pass
  *   gsa_attn_probs_mean, gsa_indexer_kl_bwd   the indexer's loss and its derivatives (Sec. 5.1, Eq. 13-14)
  *   gsa_vbar_update                        the running mean of the score variance of Eq. 8
+ * Serving from a cache of pages that holds K and V' in 4 bits (gsa_cache_*, second half of this file):
+ *   gsa_cache_reserve, gsa_cache_fork, gsa_cache_release, gsa_cache_compact   its pages
+ *   gsa_cache_append, gsa_cache_read                                          tokens in, contiguous tensors out
+ *   gsa_cache_indexer_scores, gsa_cache_topk, gsa_cache_attn_fwd              the three stages on it
  *
  * Conventions common to every call
  *   - Every data pointer is DEVICE memory owned by the caller, 16-byte aligned and
@@ -66,8 +70,9 @@ typedef enum {
     GSA_ERR_DEVICE_TIMEOUT = -5,   /* a bounded device-side wait expired (see device status) */
     GSA_ERR_STATIC_SCRATCH = -6,   /* problem larger than the built-in scratch array of the
                                       allocation-free entry point                            */
-    GSA_ERR_INDEX_RANGE = -7       /* a kernel met an index set entry outside [0, Lk) or a budget
+    GSA_ERR_INDEX_RANGE = -7,      /* a kernel met an index set entry outside [0, Lk) or a budget
                                       outside [0, k_max] (see device status)                 */
+    GSA_ERR_CACHE_FULL = -8        /* the pool has too few free pages: the call changed nothing (see device status) */
 } gsa_status;
 
 /* Hyper-parameters (Table 1 of the paper) plus the call's geometry. */
@@ -347,10 +352,123 @@ int gsa_forward_host(const gsa_params_t *p, const void *Q, const void *K, const 
                      const void *g1_logits, const void *g2_logits, void *out, int32_t *kt_out,
                      int32_t slab_rows, void *arena, size_t arena_bytes, void *stream);
 
+/* ==== A paged cache that holds K and V' in 4 bits ==========================================================================
+ *
+ * (The paper has no counterpart: this is the serving side of the path, for several sequences of different lengths.)
+ *
+ * A pool of n_pages pages of page_tokens tokens each.  table[b, s / page_tokens] is the page that holds position s of sequence
+ * b; lens[b] is the number of its tokens; refs[page] says how many table entries name the page (0: free).  Several sequences
+ * may name one page; only a sequence's last page can be partly filled, and that one is never shared.  An empty cache has
+ * table = -1, lens = 0, refs = 0 and any bytes in its pool.  All four arrays are the caller's device memory; the calls below
+ * change them on the device, in stream order, without waiting for the host, and can be captured into a graph.
+ *
+ * A token's record: D / 2 bytes of K codes, D / 2 bytes of V' codes, D / 8 scale bytes (D = n_kv * d_h), padded to a
+ * multiple of 16; behind the records of a page stand its tokens' k^I, dI bf16 each.
+ *   codes   4 bits a value, head-major, the value of even d in a byte's low half
+ *   scales  one byte for 16 consecutive values of a head: [n_kv][K, V'][d_h / 16].  Byte n stands for
+ *           s = (1 + (n % 8) / 8) * 2^(n / 8 - 20), n = 255 for NaN; a code u stands for (u - 8) * s.
+ * What is stored of 16 values x:  y = max|x| / 7,  s = y rounded to three bits behind its leading one (halves up), at least
+ * 2^-20 and at most 1.75 * 2^11,  u = 8 + (x / s rounded to the nearest integer, halves to even, clamped to -7 .. 7).  An
+ * infinity or a NaN among them makes all 16 read as NaN.  Values above 7 * 3584 saturate; a group below 2^-21 reads as zeros.
+ * A stored value has at most seven significant bits: it is exact in bf16.
+ *
+ * Supported: n_kv in {1, 2, 4, 8}; d_h in {64, 128}; dI in {32, 64}; page_tokens in {16, 32, 64, 128}; B <= 4096;
+ * n_pages <= 2^20; max_pages * page_tokens < 2^24.
+ *
+ * What the device finds wrong -- a length outside [0, max_pages * page_tokens], a table entry outside [0, n_pages) where a
+ * token is read, an index set entry outside [0, lens[b]) -- is reported through the status word (GSA_ERR_INDEX_RANGE) and
+ * never becomes an address: reads are clamped into the pool (the results of that row are then meaningless), writes are skipped.
+ */
+typedef struct gsa_cache {
+    void *pool;           /* n_pages * gsa_cache_page_bytes, 32-byte aligned                 */
+    int32_t *table;       /* [B, max_pages]                                                  */
+    int32_t *lens;        /* [B]                                                             */
+    int32_t *refs;        /* [n_pages]                                                       */
+    int32_t n_pages, page_tokens, max_pages, B;
+    int32_t n_kv, d_h, dI;
+} gsa_cache_t;
+
+/* Bytes of one page, and of the workspace that every gsa_cache_* call but gsa_cache_attn_fwd takes (host call; the pointers in
+ * *c are not looked at). */
+int gsa_cache_page_bytes(const gsa_cache_t *c, size_t *bytes);
+int gsa_cache_workspace_bytes(const gsa_cache_t *c, size_t *bytes);
+
+/*
+ * Pages for n_new[b] more tokens of every sequence: start[b] = lens[b], lens[b] += n_new[b], free pages taken lowest number
+ * first, in the order of the sequences.  All or nothing: if the pool has too few free pages, a table row is too short, or an
+ * n_new is negative, nothing changes, every start[b] is -1 (gsa_cache_append then writes nothing) and the status word says so.
+ *   n_new, start  [B] int32 on the device, distinct
+ */
+int gsa_cache_reserve(const gsa_cache_t *c, const int32_t *n_new, int32_t *start, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Stores tokens: row i < n_new[b] of K, V, kI goes to position start[b] + i of sequence b; V' = bf16(fp32(V * sigmoid(g2)))
+ * (Eq. 9; the product as if formed exactly and rounded to fp32, then to bf16, both halves to even; gsa_value_gate, which approximates
+ * the sigmoid, may differ in the last bit of V').
+ *   K, V, g2_logits [B, L_new, n_kv, d_h] bf16, 32-byte aligned, kI [B, L_new, dI] bf16; g2_logits may be NULL: V is
+ *                   taken as already gated
+ *   n_new, start    [B] int32 on the device, as given to and written by gsa_cache_reserve; rows i >= n_new[b] are not
+ *                   read, and a sequence with start[b] < 0 is left out; an n_new[b] above L_new is reported
+ * A position outside [0, lens[b]) or on a page that is shared (refs != 1) is skipped and reported.
+ */
+int gsa_cache_append(const gsa_cache_t *c, int32_t L_new, const void *K, const void *V, const void *g2_logits, const void *kI,
+                     const int32_t *n_new, const int32_t *start, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The cache as contiguous tensors, which gsa_forward and the per-stage calls take (V already gated: g2_logits = NULL): for
+ * chunked prefill of many rows against the cache.
+ *   K, V [B, L, n_kv, d_h] bf16, 32-byte aligned, kI [B, L, dI] bf16, each may be NULL; positions s >= lens[b] are left as they were
+ */
+int gsa_cache_read(const gsa_cache_t *c, int32_t L, void *K, void *V, void *kI, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Sequence b becomes a copy of sequence src_of[b] (negative: b stays as it is).  With share != 0 its full pages are shared
+ * and the partly filled last one is copied; otherwise every page is copied.  New pages are taken lowest number first, in the
+ * order of the sequences.  All or nothing, as gsa_cache_reserve: refused if pages are missing, if lens[b] != 0, if src_of[b]
+ * is not a sequence or is itself a copy of this call.
+ *   src_of  [B] int32 on the device
+ */
+int gsa_cache_fork(const gsa_cache_t *c, const int32_t *src_of, int32_t share, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Ends every sequence b with drop[b] != 0: its pages lose one reference, its table row becomes -1, its length 0.
+ *   drop    [B] int32 on the device
+ */
+int gsa_cache_release(const gsa_cache_t *c, const int32_t *drop, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Moves the pool's live pages to its front: with n live pages, the k-th live page at or behind position n takes the place of
+ * the k-th free one in front of it; table and refs follow.  live_pages[0] = n: pages from n on are free.
+ *   live_pages  one int32 on the device
+ */
+int gsa_cache_compact(const gsa_cache_t *c, int32_t *live_pages, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The three stages on the cache, for Lq query rows of every sequence, its last Lq tokens: query t of sequence b sees the keys
+ * s = 0 .. lens[b] - Lq + t (none if that is negative).  p gives Lq, the heads, the budget rule and an upper bound Lk of the
+ * lengths (a longer sequence is reported and cut there); p->B, n_kv, d_h, dI are the cache's, Lk <= max_pages * page_tokens,
+ * and q_begin / q_end are ignored.
+ *
+ * gsa_cache_indexer_scores: gsa_indexer_scores with k^I from the cache.  For few rows a sequence (decode): every row reads the
+ *   sequence's k^I by itself; B * Lq <= 65535.  scores [B, Lq, row_stride], written for the visible keys.
+ * gsa_cache_topk: gsa_adaptive_topk for those rows.  A row that sees no key gets kt = 0 and var = 0.
+ * gsa_cache_attn_fwd: gsa_sparse_gated_attn_fwd with K and V' from the cache.  Q, g1_logits, out [B, Lq, n_h, d_h] bf16,
+ *   idx [B, Lq, k_max], kt [B, Lq]; the entries of a set may stand in any order.  A row with kt = 0 is written as zeros.
+ *   Sums and softmax statistics are fp32; the probabilities are rounded to bf16 for their product with V'.
+ *   ws: gsa_cache_attn_workspace_bytes(p).  The result does not depend on scheduling.
+ */
+int gsa_cache_indexer_scores(const gsa_cache_t *c, const gsa_params_t *p, const void *qI, const float *w, const float *bI,
+                             float *scores, int64_t row_stride, void *ws, size_t ws_bytes, void *stream);
+int gsa_cache_topk(const gsa_cache_t *c, const gsa_params_t *p, const float *scores, int64_t row_stride, int32_t *idx,
+                   int32_t *kt, float *var, void *ws, size_t ws_bytes, void *stream);
+int gsa_cache_attn_workspace_bytes(const gsa_params_t *p, size_t *bytes);
+int gsa_cache_attn_fwd(const gsa_cache_t *c, const gsa_params_t *p, const void *Q, const void *g1_logits, const int32_t *idx,
+                       const int32_t *kt, void *out, void *ws, size_t ws_bytes, void *stream);
+
 /*
  * Waits for `stream`, reads the device status word at the start of `ws` into
  * *status_out (host) and returns GSA_OK, GSA_ERR_DEVICE_TIMEOUT (*status_out 1..3: copy producer,
- * MMA issuer, epilogue) or GSA_ERR_INDEX_RANGE (*status_out 6) accordingly.
+ * MMA issuer, epilogue), GSA_ERR_INDEX_RANGE (*status_out 6) or GSA_ERR_CACHE_FULL (*status_out 7) accordingly.
  * The word is cleared by every call that takes `ws`.  ws == NULL reads the status word of
  * gsa_sparse_gated_attn_fwd_static (it lives in the library's built-in array on the current device).
  */

@@ -25,7 +25,9 @@ EXPORTS = (
     "gsa_attn_bwd_workspace_bytes", "gsa_sparse_gated_attn_bwd", "gsa_vbar_update",
     "gsa_attn_probs_mean", "gsa_indexer_kl_workspace_bytes", "gsa_indexer_kl_bwd", "gsa_sparse_gated_attn_fwd_lse",
     "gsa_profile_set_timeline", "gsa_probe_gather", "gsa_probe_ex2", "gsa_debug_set_wait_limit", "gsa_value_gate",
-    "gsa_attn_tile_rows",
+    "gsa_attn_tile_rows", "gsa_cache_page_bytes", "gsa_cache_workspace_bytes", "gsa_cache_reserve", "gsa_cache_append",
+    "gsa_cache_read", "gsa_cache_fork", "gsa_cache_release", "gsa_cache_compact", "gsa_cache_indexer_scores",
+    "gsa_cache_topk", "gsa_cache_attn_workspace_bytes", "gsa_cache_attn_fwd",
 )
 
 STATIC_SCRATCH_BYTES = 32 << 20     # GSA_STATIC_SCRATCH_BYTES of include/gsa.h
@@ -250,7 +252,7 @@ def gsa_device_status(ws, stream=None) -> int:
     one of gsa_sparse_gated_attn_fwd_static."""
     v = ctypes.c_int32(0)
     rc = lib().gsa_device_status(_dp(ws), _stream(stream), ctypes.byref(v))
-    if rc not in (0, -5, -7):
+    if rc not in (0, -5, -7, -8):
         _check(rc, "gsa_device_status")
     return v.value
 
@@ -322,3 +324,142 @@ def gsa_profile_set_events(ev_begin=None, ev_selected=None, ev_end=None) -> None
     """torch.cuda.Event objects (already recorded once, so their handles exist) or None."""
     h = lambda e: ctypes.c_void_p(0 if e is None else e.cuda_event)
     lib().gsa_profile_set_events(h(ev_begin), h(ev_selected), h(ev_end))
+
+
+# ---- the paged 4-bit cache ------------------------------------------------------------------------------------------
+# A decode step makes five of these calls: their arguments are checked with as little work on the host as that takes.
+class gsa_cache_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("pool", "table", "lens", "refs")] + \
+               [(n, ctypes.c_int32) for n in ("n_pages", "page_tokens", "max_pages", "B", "n_kv", "d_h", "dI")]
+
+
+_PTR, _INT, _LONG, _SIZE = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+# what stands between the cache and (workspace, its bytes, stream)
+_CACHE_ARGS = {
+    "gsa_cache_reserve": (_PTR, _PTR), "gsa_cache_append": (_INT,) + (_PTR,) * 6, "gsa_cache_read": (_INT, _PTR, _PTR, _PTR),
+    "gsa_cache_fork": (_PTR, _INT), "gsa_cache_release": (_PTR,), "gsa_cache_compact": (_PTR,),
+    "gsa_cache_indexer_scores": (_PTR,) * 5 + (_LONG,), "gsa_cache_topk": (_PTR, _PTR, _LONG, _PTR, _PTR, _PTR),
+    "gsa_cache_attn_fwd": (_PTR,) * 6,
+}
+_cache_fns = {}
+
+
+def _cache_fn(name: str):
+    f = _cache_fns.get(name)
+    if f is None:
+        # (an object of its own: its argument types are nobody else's)
+        f = ctypes.CFUNCTYPE(_INT, _PTR, *_CACHE_ARGS[name], _PTR, _SIZE, _PTR)((name, lib()))
+        _cache_fns[name] = f
+    return f
+
+
+def cache_geometry(*, B: int, n_pages: int, page_tokens: int, max_pages: int, n_kv: int, d_h: int, dI: int) -> gsa_cache_t:
+    """A cache without its arrays, for the size queries."""
+    return gsa_cache_t(None, None, None, None, n_pages, page_tokens, max_pages, B, n_kv, d_h, dI)
+
+
+def make_cache(pool, table, lens, refs, *, page_tokens: int, n_kv: int, d_h: int, dI: int) -> gsa_cache_t:
+    """pool: uint8, n_pages * gsa_cache_page_bytes; table [B, max_pages], lens [B], refs [n_pages]: int32.  An empty cache has
+    table = -1, lens = 0, refs = 0.  The returned handle keeps the tensors alive."""
+    if table.dim() != 2 or lens.shape != table.shape[:1] or refs.dim() != 1:
+        raise GsaError("table is [B, max_pages], lens [B], refs [n_pages]")
+    c = cache_geometry(B=table.shape[0], n_pages=refs.numel(), page_tokens=page_tokens, max_pages=table.shape[1], n_kv=n_kv, d_h=d_h, dI=dI)
+    if pool.numel() != refs.numel() * gsa_cache_page_bytes(c):
+        raise GsaError(f"the pool has {pool.numel()} bytes, {refs.numel()} pages take {refs.numel() * gsa_cache_page_bytes(c)}")
+    if len({t.device for t in (pool, table, lens, refs)}) != 1:
+        raise GsaError("a cache lives on one device")
+    c.pool, c.table, c.lens, c.refs = _dp(pool, torch.uint8), _dp(table, I32), _dp(lens, I32), _dp(refs, I32)
+    c.tensors, c.device, c.ref = (pool, table, lens, refs), pool.get_device(), ctypes.addressof(c)
+    return c
+
+
+def _at(t, dtype, shape, device: int):
+    """Address of a contiguous tensor of that type and shape on that device; None for None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise GsaError(f"expected a contiguous {dtype} tensor {tuple(shape)} on GPU {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _cache_call(name: str, c: gsa_cache_t, ws, stream, *args) -> None:
+    if torch.cuda.current_device() != c.device or ws.get_device() != c.device or not ws.is_contiguous():
+        raise GsaError("the cache, a contiguous workspace and the current device belong together")
+    if stream is None:
+        stream = torch.cuda.current_stream()
+    rc = _cache_fn(name)(c.ref, *args, ws.data_ptr(), ws.nbytes, stream.cuda_stream)
+    if rc:
+        _check(rc, name)
+
+
+def gsa_cache_page_bytes(c: gsa_cache_t) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().gsa_cache_page_bytes(ctypes.byref(c), ctypes.byref(n)), "gsa_cache_page_bytes")
+    return n.value
+
+
+def gsa_cache_workspace_bytes(c: gsa_cache_t) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().gsa_cache_workspace_bytes(ctypes.byref(c), ctypes.byref(n)), "gsa_cache_workspace_bytes")
+    return n.value
+
+
+def gsa_cache_attn_workspace_bytes(p: gsa_params_t) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().gsa_cache_attn_workspace_bytes(ctypes.byref(p), ctypes.byref(n)), "gsa_cache_attn_workspace_bytes")
+    return n.value
+
+
+def gsa_cache_reserve(c, n_new, start, ws, stream=None) -> None:
+    """Pages for n_new[b] more tokens of every sequence; start[b] receives where they go (-1: refused, see gsa_device_status)."""
+    _cache_call("gsa_cache_reserve", c, ws, stream, _at(n_new, I32, (c.B,), c.device), _at(start, I32, (c.B,), c.device))
+
+
+def gsa_cache_append(c, K, V, g2, kI, n_new, start, ws, stream=None) -> None:
+    """Row i < n_new[b] of K, V * sigmoid(g2) and kI to position start[b] + i of sequence b (g2 None: V already gated)."""
+    d, B, L = c.device, c.B, K.shape[1]
+    kv = (B, L, c.n_kv, c.d_h)
+    _cache_call("gsa_cache_append", c, ws, stream, L, _at(K, BF16, kv, d), _at(V, BF16, kv, d), _at(g2, BF16, kv, d),
+                _at(kI, BF16, (B, L, c.dI), d), _at(n_new, I32, (B,), d), _at(start, I32, (B,), d))
+
+
+def gsa_cache_read(c, K, V, kI, ws, stream=None) -> None:
+    """The cache as contiguous tensors [B, L, ...]; any of the three may be None; positions behind a sequence's end stay as they were."""
+    L = next(t for t in (K, V, kI) if t is not None).shape[1]
+    kv = (c.B, L, c.n_kv, c.d_h)
+    _cache_call("gsa_cache_read", c, ws, stream, L, _at(K, BF16, kv, c.device), _at(V, BF16, kv, c.device),
+                _at(kI, BF16, (c.B, L, c.dI), c.device))
+
+
+def gsa_cache_fork(c, src_of, share: bool, ws, stream=None) -> None:
+    """Sequence b becomes a copy of sequence src_of[b] (negative: stays); share: full pages are shared instead of copied."""
+    _cache_call("gsa_cache_fork", c, ws, stream, _at(src_of, I32, (c.B,), c.device), 1 if share else 0)
+
+
+def gsa_cache_release(c, drop, ws, stream=None) -> None:
+    """Ends every sequence b with drop[b] != 0."""
+    _cache_call("gsa_cache_release", c, ws, stream, _at(drop, I32, (c.B,), c.device))
+
+
+def gsa_cache_compact(c, live_pages, ws, stream=None) -> None:
+    """Moves the live pages to the pool's front; live_pages (one int32) receives their number."""
+    _cache_call("gsa_cache_compact", c, ws, stream, _at(live_pages, I32, (1,), c.device))
+
+
+def gsa_cache_indexer_scores(c, p, qI, w, bI, scores, row_stride: int, ws, stream=None) -> None:
+    d, B, Lq, HI = c.device, p.B, p.Lq, p.HI
+    _cache_call("gsa_cache_indexer_scores", c, ws, stream, ctypes.addressof(p), _at(qI, BF16, (B, Lq, HI, p.dI), d),
+                _at(w, F32, (B, Lq, HI), d), _at(bI, F32, (HI,), d), _at(scores, F32, (B, Lq, row_stride), d), row_stride)
+
+
+def gsa_cache_topk(c, p, scores, row_stride: int, idx, kt, var, ws, stream=None) -> None:
+    d, rows = c.device, (p.B, p.Lq)
+    _cache_call("gsa_cache_topk", c, ws, stream, ctypes.addressof(p), _at(scores, F32, rows + (row_stride,), d), row_stride,
+                _at(idx, I32, rows + (p.k_max,), d), _at(kt, I32, rows, d), _at(var, F32, rows, d))
+
+
+def gsa_cache_attn_fwd(c, p, Q, g1, idx, kt, out, ws, stream=None) -> None:
+    d, rows = c.device, (p.B, p.Lq)
+    heads = rows + (p.n_h, p.d_h)
+    _cache_call("gsa_cache_attn_fwd", c, ws, stream, ctypes.addressof(p), _at(Q, BF16, heads, d), _at(g1, BF16, heads, d),
+                _at(idx, I32, rows + (p.k_max,), d), _at(kt, I32, rows, d), _at(out, BF16, heads, d))

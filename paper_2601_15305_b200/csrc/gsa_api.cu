@@ -100,15 +100,6 @@ cudaError_t launch_indexer(const gsa_params_t& p, RowRange rr, const __nv_bfloat
     return launch_indexer_simple(p, rr, qI, kI, w, bI, scores, row_stride, st);
 }
 
-namespace {
-
-inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline bool one_of(int v, std::initializer_list<int> l) {
-    for (int x : l) if (x == v) return true;
-    return false;
-}
-
 int check_params(const gsa_params_t* p) {
     if (!p) return GSA_ERR_INVALID_ARG;
     if (p->B < 1 || p->Lq < 1 || p->Lk < p->Lq || p->n_h < 1 || p->n_kv < 1) return GSA_ERR_INVALID_ARG;
@@ -126,6 +117,14 @@ int check_params(const gsa_params_t* p) {
     if ((int64_t)p->B * p->Lq >= (1ll << 31)) return GSA_ERR_UNSUPPORTED_SHAPE;
     return GSA_OK;
 }
+
+int cuda_rc(cudaError_t e) {
+    if (e == cudaSuccess) return GSA_OK;
+    fprintf(stderr, "gsa: CUDA error: %s\n", cudaGetErrorString(e));
+    return GSA_ERR_CUDA;
+}
+
+namespace {
 
 int row_range(const gsa_params_t* p, RowRange* rr) {
     const int qe = p->q_end <= 0 ? p->Lq : p->q_end;
@@ -167,12 +166,6 @@ WsPlan plan_ws(const gsa_params_t& p, int32_t slab_rows) {
     w.attn_off = off; off += align_up(attn_scratch_bytes(p), 256);
     w.total = off;
     return w;
-}
-
-int cuda_rc(cudaError_t e) {
-    if (e == cudaSuccess) return GSA_OK;
-    fprintf(stderr, "gsa: CUDA error: %s\n", cudaGetErrorString(e));
-    return GSA_ERR_CUDA;
 }
 
 }  // namespace
@@ -702,7 +695,7 @@ int gsa_device_status(const void* ws, void* stream, int32_t* status_out) {
     if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_rc(e);
     if (status_out) *status_out = v;
-    return v == kDevOk ? GSA_OK : (v == kDevBadIndex ? GSA_ERR_INDEX_RANGE : GSA_ERR_DEVICE_TIMEOUT);
+    return v == kDevOk ? GSA_OK : v == kDevBadIndex ? GSA_ERR_INDEX_RANGE : v == kDevCacheFull ? GSA_ERR_CACHE_FULL : GSA_ERR_DEVICE_TIMEOUT;
 }
 
 int gsa_attn_tile_rows(const gsa_params_t* p, int32_t* fwd_rows, int32_t* bwd_tiles) {
@@ -762,6 +755,7 @@ const char* gsa_status_string(int s) {
         case GSA_ERR_CUDA: return "CUDA error";
         case GSA_ERR_DEVICE_TIMEOUT: return "a bounded device-side wait expired";
         case GSA_ERR_INDEX_RANGE: return "an index set entry or a budget was out of range (clamped or skipped on the device)";
+        case GSA_ERR_CACHE_FULL: return "the cache's pool has too few free pages";
         case GSA_ERR_STATIC_SCRATCH: return "problem exceeds the built-in scratch array (GSA_STATIC_SCRATCH_BYTES)";
     }
     return "unknown status";

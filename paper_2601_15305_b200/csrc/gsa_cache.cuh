@@ -1,0 +1,56 @@
+// The paged 4-bit cache (include/gsa.h) as the kernels see it.
+#pragma once
+
+#include "gsa_common.cuh"
+
+namespace gsa {
+
+struct CacheView {
+    unsigned char* pool;
+    int32_t *table, *lens, *refs;
+    int64_t page_bytes;
+    int32_t n_pages, T, log_t, max_pages, B;
+    int32_t n_kv, d_h, dI;
+    int32_t rec;                 // bytes of a token's record: D / 2 K codes, D / 2 V' codes, D / 8 scales, padding (D = n_kv * d_h)
+    int32_t keys_off;            // where a page's k^I start: T * rec
+};
+
+constexpr int kCacheGroup = 16;  // values that share a scale
+// A scale byte n is the top of an fp32 number's bits: exponent field 107 + n / 8 (2^(n / 8 - 20)) and three bits of the mantissa.
+constexpr uint32_t kScaleBias = 107u << 3;
+constexpr uint32_t kScaleNan = 255u;
+// the same in bf16: (byte << 4) + kScaleBiasBf16
+constexpr uint32_t kScaleBiasBf16 = kScaleBias << 4;
+
+// tokens of sequence b, at most `cap`; `bad` is raised by a length outside [0, cap]
+__device__ __forceinline__ int32_t checked_len(const CacheView& c, int32_t b, int32_t cap, bool& bad) {
+    const int32_t n = __ldg(c.lens + b);
+    bad |= n < 0 || n > cap;
+    return min(max(n, 0), cap);
+}
+// page of position s (inside the table's row) of sequence b; `bad` is raised, and page 0 taken, by an entry that names none
+__device__ __forceinline__ int32_t checked_page(const CacheView& c, int32_t b, int32_t s, bool& bad) {
+    const int32_t page = __ldg(c.table + (int64_t)b * c.max_pages + (s >> c.log_t));
+    if ((uint32_t)page < (uint32_t)c.n_pages) return page;
+    bad = true;
+    return 0;
+}
+
+// ---- launchers -------------------------------------------------------------------------------------------------------------
+size_t cache_page_list_bytes(const CacheView& c);        // scratch of the page calls behind the status head
+cudaError_t launch_cache_reserve(const CacheView& c, const int32_t* n_new, int32_t* start, int32_t* ws, cudaStream_t st);
+cudaError_t launch_cache_fork(const CacheView& c, const int32_t* src_of, bool share, int32_t* ws, cudaStream_t st);
+cudaError_t launch_cache_release(const CacheView& c, const int32_t* drop, int32_t* dev_status, cudaStream_t st);
+cudaError_t launch_cache_compact(const CacheView& c, int32_t* live_pages, int32_t* ws, cudaStream_t st);
+cudaError_t launch_cache_append(const CacheView& c, int32_t L_new, const __nv_bfloat16* K, const __nv_bfloat16* V,
+                                const __nv_bfloat16* g2, const __nv_bfloat16* kI, const int32_t* n_new, const int32_t* start,
+                                int32_t* dev_status, cudaStream_t st);
+cudaError_t launch_cache_read(const CacheView& c, int32_t L, __nv_bfloat16* K, __nv_bfloat16* V, __nv_bfloat16* kI,
+                              int32_t* dev_status, cudaStream_t st);
+cudaError_t launch_cache_indexer(const CacheView& c, const gsa_params_t& p, RowRange rr, const __nv_bfloat16* qI, const float* w,
+                                 const float* bI, float* scores, int64_t row_stride, int32_t* dev_status, cudaStream_t st);
+size_t cache_attn_scratch_bytes(const gsa_params_t& p);
+cudaError_t launch_cache_attn(const CacheView& c, const gsa_params_t& p, const __nv_bfloat16* Q, const __nv_bfloat16* g1,
+                              const int32_t* idx, const int32_t* kt, __nv_bfloat16* out, int32_t* ws, cudaStream_t st);
+
+}  // namespace gsa

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <initializer_list>
 
 #include "gsa.h"
 
@@ -37,8 +38,8 @@ enum : int32_t { kGeneralSets = 1,       // an index set that a bit mask cannot 
 constexpr int kStatusPairsWord = 4;      // two words (64 bits): CTAs of the mask builder and selected pairs that they have counted
 
 // device status word values: which bounded wait of a tensor-core pipeline ran out (copy producer, MMA
-// issuer, epilogue), or that a kernel met an index set entry / budget outside its range
-enum : int32_t { kDevOk = 0, kDevTimeoutTma = 1, kDevTimeoutMma = 2, kDevTimeoutEpi = 3, kDevBadIndex = 6 };
+// issuer, epilogue), that a kernel met an index set entry / budget outside its range, or that a cache's pool has too few free pages
+enum : int32_t { kDevOk = 0, kDevTimeoutTma = 1, kDevTimeoutMma = 2, kDevTimeoutEpi = 3, kDevBadIndex = 6, kDevCacheFull = 7 };
 
 // Status word of the call this host thread is enqueueing: the entry point sets it (the head of the call's
 // workspace, or null when the call has none) and the launchers copy it into their kernels' arguments.
@@ -86,6 +87,17 @@ enum : int32_t { kStageIndexer = 0, kStageSelect = 1, kStageValueGate = 2, kStag
                  kStageFinalize = 5, kStageTiles = 6 };
 void timeline_mark(int32_t stage, cudaStream_t st);
 
+// ---- argument checks shared by the entry points (gsa_api.cu) ---------------------------------
+int check_params(const gsa_params_t* p);
+int cuda_rc(cudaError_t e);                                // gsa_status of a CUDA error, which is named on stderr
+inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned32(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0; }
+inline bool one_of(int v, std::initializer_list<int> l) {
+    for (int x : l) if (x == v) return true;
+    return false;
+}
+
 // ---- stage launchers (host) ----------------------------------------------------------------
 cudaError_t launch_indexer(const gsa_params_t& p, RowRange rr, const __nv_bfloat16* qI,
                            const __nv_bfloat16* kI, const float* w, const float* bI, float* scores,
@@ -93,7 +105,8 @@ cudaError_t launch_indexer(const gsa_params_t& p, RowRange rr, const __nv_bfloat
 
 cudaError_t launch_select(const gsa_params_t& p, RowRange rr, const float* scores,
                           int64_t row_stride, int32_t* idx, int32_t* kt, float* var,
-                          IdxLayout il, int32_t* fallback_rows /*nullable counter*/, cudaStream_t st);
+                          IdxLayout il, int32_t* fallback_rows /*nullable counter*/, cudaStream_t st,
+                          const int32_t* lens = nullptr /*[B] on the device: keys of each sequence, at most Lk, instead of Lk*/);
 
 cudaError_t launch_value_gate(const __nv_bfloat16* V, const __nv_bfloat16* g2, __nv_bfloat16* Vg,
                               int64_t n_elems, cudaStream_t st, int32_t* untileable = nullptr /*raised if a gated value is*/,

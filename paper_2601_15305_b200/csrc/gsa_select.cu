@@ -56,7 +56,24 @@ struct SelectArgs {
     int32_t Lq, Lk;
     int32_t k_base, k_min, k_max, k_mode;
     float v_bar;
+    const int32_t* lens;      // keys of each sequence instead of Lk (nullable); a launch then does the rows that see
+    int32_t n_lo, n_hi;       // n_lo < n <= n_hi keys, and those that see none if n_lo is 0
 };
+
+// visible keys of a row; false if the row belongs to another launch or, seeing nothing, has just been written
+__device__ __forceinline__ bool row_keys(const SelectArgs& a, int b, int t, int32_t* out_idx, int64_t orow, bool writer, int& n) {
+    n = a.Lk - a.Lq + t + 1;
+    if (!a.lens) return true;
+    n = min(max(__ldg(a.lens + b), 0), a.Lk) - a.Lq + t + 1;
+    if (n <= 0 && a.n_lo == 0 && writer) {
+        for (int i = threadIdx.x; i < a.k_max; i += blockDim.x) out_idx[i] = -1;
+        if (threadIdx.x == 0) {
+            a.kt[orow] = 0;
+            if (a.var) a.var[orow] = 0.f;
+        }
+    }
+    return n > a.n_lo && n <= a.n_hi;
+}
 
 // monotone map fp32 -> uint32 (larger float <=> larger key); -0 is folded onto +0, and the sum makes every NaN the same
 // one: key 0xFFFFFFFF, above all others.  (-inf has key 0x007FFFFF: no score has key 0.)
@@ -223,10 +240,11 @@ __global__ void __launch_bounds__(kSelThreads, 2) gsa_select_kernel(const Select
     const int b = a.rr.b0 + (int)blockIdx.x / q_rows;
     const int t = q_first + (int)blockIdx.x % q_rows;
     const int lr = (b - a.rr.b0) * a.rr.R + (t - a.rr.q_begin);
-    const int n = a.Lk - a.Lq + t + 1;                       // visible keys
     const float* __restrict__ grow = a.scores + (int64_t)lr * a.row_stride;
     const int64_t orow = a.il.row(b, t);
     int32_t* __restrict__ out_idx = a.idx + orow * a.k_max;
+    int n;                                                   // visible keys
+    if (!row_keys(a, b, t, out_idx, orow, true, n)) return;
     const int nchunks = (n + kIter - 1) / kIter;              // chunks of 512 consecutive scores (long rows)
     const bool listed = nchunks <= kMaxChunks;  // longer rows go straight to the whole-row path
     // the table of list segments has one entry per 128 scores (8 lanes of an iteration) while that fits,
@@ -623,17 +641,18 @@ __global__ void __launch_bounds__(NT, 1024 / NT) gsa_select_short_kernel(const S
         if constexpr (CS > 1) cg::this_cluster().sync();
         else __syncthreads();
     };
-    if constexpr (CS > 1) cg::this_cluster().barrier_arrive();        // (awaited before the first access to another CTA's memory)
     const int bl = item / q_rows;
     const int t = q_first + q_rows - 1 - item % q_rows;       // long rows first
     const int lr = bl * a.rr.R + (t - a.rr.q_begin);
-    const int n_row = a.Lk - a.Lq + t + 1;                    // visible keys, at most 32 NT CS
+    const int64_t orow = a.il.row(a.rr.b0 + bl, t);
+    int32_t* __restrict__ out_idx = a.idx + orow * a.k_max;
+    int n_row;                                                // visible keys, at most 32 NT CS
+    if (!row_keys(a, a.rr.b0 + bl, t, out_idx, orow, rank == 0, n_row)) return;       // (the same for all CTAs of a cluster)
+    if constexpr (CS > 1) cg::this_cluster().barrier_arrive();        // (awaited before the first access to another CTA's memory)
     const int slice = CS > 1 ? ((n_row + CS - 1) / CS + 127) / 128 * 128 : n_row;
     const int p0 = rank * slice;                              // this CTA's first position, and how many it has
     const int n = CS > 1 ? max(0, min(slice, n_row - p0)) : n_row;
     const float* __restrict__ grow = a.scores + (int64_t)lr * a.row_stride + p0;
-    const int64_t orow = a.il.row(a.rr.b0 + bl, t);
-    int32_t* __restrict__ out_idx = a.idx + orow * a.k_max;
 
     // ---- the slice: moments in fp64, range of the keys ----
     // (a score past the end is 0 in the moments and has key 0, which no score has: below every threshold and outside every
@@ -924,7 +943,7 @@ cudaError_t launch_all_visible(const gsa_params_t& p, RowRange rr, int32_t* idx,
 
 cudaError_t launch_select(const gsa_params_t& p, RowRange rr, const float* scores,
                           int64_t row_stride, int32_t* idx, int32_t* kt, float* var, IdxLayout il,
-                          int32_t* fallback_rows, cudaStream_t st) {
+                          int32_t* fallback_rows, cudaStream_t st, const int32_t* lens) {
     if (rr.rows() <= 0) return cudaSuccess;
     SelectArgs a;
     a.scores = scores; a.row_stride = row_stride; a.idx = idx; a.kt = kt; a.var = var;
@@ -932,8 +951,28 @@ cudaError_t launch_select(const gsa_params_t& p, RowRange rr, const float* score
     a.rr = rr; a.il = il; a.Lq = p.Lq; a.Lk = p.Lk;
     a.k_base = p.k_base; a.k_min = p.k_min; a.k_max = p.k_max; a.k_mode = p.k_mode; a.v_bar = p.v_bar;
 
+    a.lens = lens; a.n_lo = 0; a.n_hi = INT32_MAX;
+    const size_t smem = ((sizeof(SelShared) + 15) / 16) * 16;
+
     // rows by the number of scores they see: up to 4096, 8192, 16384, longer
     const int off = p.Lk - p.Lq;
+    if (lens) {                                               // (known on the device only: the longest that a row may be decides)
+        const int q0 = rr.q_begin, n_max = off + q0 + rr.R;
+        if (n_max <= 4096) return launch_short<128, 1>(a, q0, rr.R, st);
+        if (n_max <= 8192) return launch_short<256, 1>(a, q0, rr.R, st);
+        if (n_max <= 16384) return launch_short<512, 1>(a, q0, rr.R, st);
+        if (n_max <= 32 * 512 * kRowCluster && (int64_t)rr.rows() * kRowCluster <= 2 * sm_count())
+            return launch_short<512, kRowCluster>(a, q0, rr.R, st);
+        a.n_hi = 16384;
+        cudaError_t e = launch_short<512, 1>(a, q0, rr.R, st);
+        if (e != cudaSuccess) return e;
+        a.n_lo = 16384; a.n_hi = INT32_MAX;
+        e = cudaFuncSetAttribute(gsa_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+        launch_chained(gsa_select_kernel, rr.rows(), kSelThreads, smem, st, a, q0, rr.R);
+        ++g_launches;
+        return cudaGetLastError();
+    }
     auto first_longer = [&](int cap) {                        // first query row that sees more than cap keys, within the range
         const int t = cap - off;
         return t < rr.q_begin ? rr.q_begin : (t > rr.q_begin + rr.R ? rr.q_begin + rr.R : t);
@@ -947,7 +986,6 @@ cudaError_t launch_select(const gsa_params_t& p, RowRange rr, const float* score
     // few long rows: a cluster each, while all of them fit the GPU at once
     if (off + t_end <= 32 * 512 * kRowCluster && (int64_t)rr.nb * (t_end - t16) * kRowCluster <= 2 * sm_count())
         return launch_short<512, kRowCluster>(a, t16, t_end - t16, st);
-    const size_t smem = ((sizeof(SelShared) + 15) / 16) * 16;
     // (set on every call: the attribute belongs to the current device)
     e = cudaFuncSetAttribute(gsa_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;

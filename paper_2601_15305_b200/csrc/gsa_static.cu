@@ -43,7 +43,6 @@ cudaError_t scratch_on_current_device(void** ptr) {
     return cudaSuccess;
 }
 
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 }  // namespace
 
