@@ -385,9 +385,9 @@ def _at(t, dtype, shape, device: int):
 def _cache_call(name: str, c: gsa_cache_t, ws, stream, *args) -> None:
     if torch.cuda.current_device() != c.device or ws.get_device() != c.device or not ws.is_contiguous():
         raise GsaError("the cache, a contiguous workspace and the current device belong together")
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    rc = _cache_fn(name)(c.ref, *args, ws.data_ptr(), ws.nbytes, stream.cuda_stream)
+    # (torch.cuda.current_stream() makes an object: 3 us, a fifth of a call)
+    st = torch._C._cuda_getCurrentRawStream(c.device) if stream is None else stream.cuda_stream
+    rc = _cache_fn(name)(c.ref, *args, ws.data_ptr(), ws.nbytes, st)
     if rc:
         _check(rc, name)
 

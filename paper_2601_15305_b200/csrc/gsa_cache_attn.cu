@@ -2,28 +2,34 @@
 //
 // A set is walked in tiles of 16 keys; n_kv warps (a unit) take a tile together, one KV head each.  As in gsa_attn.cu keys are the
 // M side of an MMA and the group's query heads its N side, and a contraction does not care about the order of its index, so a lane takes
-// the codes that lie together in memory:
+// the codes that lie together in memory.  What a tile costs is taking the codes apart, so as little as possible is done to them:
 //   K   lane (gid, tig): the tig-th quarter of the head row of keys gid and gid + 8, eight codes a word; Q is read with the same
-//       permutation.                                                               S^T[key, head] = K[key, :] . Q[head, :]
+//       permutation.  A code u, masked out of its word, IS the fp16 number u * 2^-24 (16 u * 2^-24 in a half word's second place, with
+//       Q / 16 against it), and that is the operand: one logical operation for two codes.
+//       Scales: in a k-step each of the four lanes of a key has codes of a group of its own.  Up to four query heads leave columns of
+//       the MMA free, and those keep the four lanes' groups apart: column (slot, head) of Q^T has Q[head] where lane `slot` supplies
+//       the index and 0 elsewhere.  The accumulators are then sums over one group each, Sum u q; their scales (which that lane holds)
+//       and the code's offset (-8 Sum q, what the accumulators start from) are applied to them, and the slots are added up by
+//       shuffles.                                                                S^T[key, head] = K[key, :] . Q[head, :]
+//       (Q as fp16: a power of two brings the warp's largest |q| to 2^14 .. 2^15, where every bf16 within 2^-25 of it is exact.)
+//       Eight heads fill the columns: there K is dequantised, in bf16, by one multiply-add, (128 + u) s - 136 s, exactly.
 //   V'  lane (gid, tig): the gid-th eighth of keys 2 tig, 2 tig + 1, 2 tig + 8, 2 tig + 9; words of two keys are joined half by half, so
 //       that a code position yields the pair (key, key + 1) of one d.                O^T[d, head] += V'^T[d, key] P^T[key, head]
-//       At d_h = 128 that eighth is one group of 16 and has one scale.
-//   dequantising K  one logical operation puts a code into the mantissa of 128 (bf16), one multiply-add by (s, -136 s) gives code * s,
-//       exactly: (128 + u) s - 136 s has at most seven significant bits, 136 s at most eight.
-//   dequantising V'  in fp16, whose longer mantissa takes codes at two places of a half word without a shift: (1024 + u) - 1032 or
-//       (1024 + 16 u) / 16 - 72, then times s.  Every value of the format is exact in fp16 too (105 * 2^-23 .. 7 * 3584).
+//       At d_h = 128 that eighth is one group of 16 and has one scale.  In fp16 (1024 + u) - 1032, or (1024 + 16 u) / 16 - 72, then
+//       times s: every value of the format is exact in fp16 too (105 * 2^-23 .. 7 * 3584).
 // The tile's numerators are rounded to fp16 for the second product.  They are taken against a reference that leaves a row's largest
 // between 2^7 and 2^15, so that rounding is at most 2^-11 of a numerator, or 2^-25 where that is less than fp16's normal range goes down
 // to: 2^-32 of the row's sum.  (In bf16, 2^-8 of each, the error of the 32 x 128K case against 64 bits is 2.3e-3; with fp16 it is
 // 1.7e-3, the output's own rounding.)  Statistics, scores and sums are fp32.
 //
 // Records come by asynchronous copies into a ring of kStages tiles a warp (2304 bytes each at d_h = 128), so that some 100 KB of an SM
-// are in flight; indices are read two tiles ahead of that, pages one.
+// are in flight.  Indices and pages are looked up for blocks of four or eight tiles, each warp of a unit a share of the keys, two blocks
+// ahead; the records' addresses pass through shared memory.
 //
 // Work split: the tiles of all rows, one after another, are dealt to the units in equal runs, whatever the sets' sizes (each CTA sums
 // up the budgets for itself).  A row that lies within one unit's run is finished there; the others' parts (at most two a unit) go to
-// the workspace as softmax state and are merged by a second kernel, in order, so that nothing depends on scheduling.  With more rows than
-// kMaxSplitRows a unit takes whole rows in turn instead.
+// the workspace as softmax state and are merged by a second kernel, in order, so that nothing depends on scheduling.  More rows than
+// kMaxSplitRows take several such launches.
 #include "gsa_cache.cuh"
 
 #include <cuda_fp16.h>
@@ -36,7 +42,8 @@ constexpr int kWarps = 8;
 constexpr int kTile = 16;                  // keys
 constexpr int kStages = 4;                 // tiles of a warp's ring: one being computed on, the others in flight
 constexpr int kMinTiles = 2;               // fewest tiles worth a unit of their own
-constexpr int kMaxSplitRows = 2048;        // rows whose budgets a CTA sums up (16 KB of its shared memory)
+constexpr int kMaxSplitRows = 2048;        // rows of one launch, whose budgets a CTA sums up (16 KB of its shared memory)
+constexpr int kAddressBlocks = 3;          // blocks of record addresses: being read, next, being written
 constexpr int kCtasPerSm = 2;
 constexpr int kMergeWarps = 8;
 constexpr float kRefUnder = 7.0f;          // a new softmax reference lies 2^7 under the score that moved it there,
@@ -47,7 +54,7 @@ struct CacheAttnArgs {
     const __nv_bfloat16 *Q, *g1;
     const int32_t *idx, *kt;
     __nv_bfloat16* out;
-    int32_t rows, Lq, Lk, n_h, k_max;
+    int32_t rows, row0, Lq, Lk, n_h, k_max;            // rows of this launch, the first one's number in the call
     float scale_log2;
     int32_t units;                         // of the launch; as many as there are tiles for take part
     float* state;                          // [2 * units][n_h][d_h] numerators
@@ -178,44 +185,50 @@ struct Stage {
     static constexpr int kV = kTile * kRow, kS = kV + kTile * kVRow, kBytes = kS + kTile * kSRow;
 };
 __host__ __device__ constexpr size_t row_table_bytes(int rows) { return ((size_t)(2 * rows + 1) * 4 + 15) / 16 * 16; }
+// tiles of a block of addresses: one or two keys a lane of the unit's warps
+constexpr int block_tiles(int NKV) { return NKV >= 4 ? 8 : 4; }
+constexpr size_t address_bytes(int NKV) { return (size_t)(kWarps / NKV) * kAddressBlocks * block_tiles(NKV) * kTile * 8; }
+template <int DH, int NKV>
+constexpr size_t fixed_smem() { return address_bytes(NKV) + (size_t)kWarps * kStages * Stage<DH>::kBytes; }
 
-template <int DH, int G, bool SPLIT>
+template <int DH, int G, int NKV>
 __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) gsa_cache_attn_kernel(const CacheAttnArgs a) {
     chain_wait();
     using St = Stage<DH>;
+    constexpr int D = NKV * DH;
     constexpr int KW = DH / 32;            // words of K codes a lane has of a key
     constexpr int VW = DH / 64;            // words of V' codes a lane has of a key
-    constexpr int KS = DH / 64;            // scale bytes of those K codes
+    constexpr int KS = DH / 64;            // scales of those K codes
     constexpr int MT = DH / 16;
     constexpr int DL = DH / 8;             // consecutive d of O that a lane holds, for heads 2 tig and 2 tig + 1
     constexpr int CPK = DH / 32, KPI = 32 / CPK;       // 16-byte chunks of a key's codes, keys that one copy of a warp covers
-    extern __shared__ __align__(16) unsigned char smem[];  // SPLIT: cum[rows + 1], budget[rows]; the rings
+    constexpr int SUBS = kWarps / NKV;
+    constexpr int BT = block_tiles(NKV), KPW = BT * kTile / NKV, STEPS = (KPW + 31) / 32;      // keys of a block that a warp looks up
+    constexpr bool COLS = G <= 4;          // groups in columns of their own
+    constexpr int SETS = G == 4 ? 2 : 1;   // MMAs that the four slots take
+    extern __shared__ __align__(16) unsigned char smem[];  // record addresses, rings, cum[rows + 1], budget[rows]
     __shared__ int32_t warp_sum[kWarps];
     __shared__ int32_t cta_bad;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int gid = lane >> 2, tig = lane & 3;
     const CacheView& c = a.c;
-    const int n_kv = c.n_kv, subs = kWarps / n_kv;
-    const int h = warp & (n_kv - 1);
-    const int unit = (warp / n_kv) * gridDim.x + blockIdx.x;
-    int32_t* cum = reinterpret_cast<int32_t*>(smem);
-    int32_t* budget = cum + a.rows + 1;
-    const uint32_t ring = smem_u32(smem) + (SPLIT ? (uint32_t)row_table_bytes(a.rows) : 0u) + warp * (kStages * St::kBytes);
+    const int h = warp % NKV, sub = warp / NKV;
+    const int unit = sub * gridDim.x + blockIdx.x;
+    int64_t* const addresses = reinterpret_cast<int64_t*>(smem) + sub * (kAddressBlocks * BT * kTile);
+    const uint32_t ring = smem_u32(smem) + (uint32_t)address_bytes(NKV) + warp * (kStages * St::kBytes);
+    int32_t* const cum = reinterpret_cast<int32_t*>(smem + fixed_smem<DH, NKV>());
+    int32_t* const budget = cum + a.rows + 1;
     bool bad = false;
-    auto budget_of = [&](int32_t row) -> int32_t {
-        const int32_t k = __ldg(a.kt + row);
-        bad |= k < 0 || k > a.k_max;
-        return clamp_budget(k, a.k_max);
-    };
     if (threadIdx.x == 0) cta_bad = 0;
 
-    int32_t tiles = 0, units = gridDim.x * subs;
-    if constexpr (SPLIT) {
-        // ---- tiles in front of every row ----
+    // ---- tiles in front of every row ----
+    int32_t tiles = 0;
+    {
         const int per = (a.rows + kWarps * 32 - 1) / (kWarps * 32), r0 = min(a.rows, (int)threadIdx.x * per), r1 = min(a.rows, r0 + per);
         int32_t mine = 0;
         for (int r = r0; r < r1; ++r) {
-            const int32_t k = budget_of(r);
+            const int32_t given = __ldg(a.kt + r), k = clamp_budget(given, a.k_max);
+            bad |= given != k;
             budget[r] = k;
             mine += (k + kTile - 1) / kTile;
         }
@@ -238,297 +251,383 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) gsa_cache_attn_kernel
             at += (budget[r] + kTile - 1) / kTile;
         }
         if (threadIdx.x == 0) cum[a.rows] = tiles;
-        units = units_for(tiles, units);
+        __syncthreads();
     }
-    __syncthreads();
-    int32_t lo = 0, hi = 0;                // SPLIT: this unit's tiles
-    bool works = true;
-    if constexpr (SPLIT) {
-        works = unit < units;
-        if (works) {
-            lo = first_tile(unit, tiles, units);
-            hi = first_tile(unit + 1, tiles, units);
-        }
+    const int32_t units = units_for(tiles, gridDim.x * SUBS);
+    int32_t lo = 0, n = 0;                 // this unit's tiles: lo .. lo + n - 1
+    if (unit < units) {
+        lo = first_tile(unit, tiles, units);
+        n = first_tile(unit + 1, tiles, units) - lo;
     }
+    if (n > 0) {
+        int32_t row = 0;                   // the row that holds tile lo (of rows that start there the last: the others are empty)
+        for (int32_t rh = a.rows - 1; row < rh;) {
+            const int32_t m = (row + rh + 1) >> 1;
+            if (cum[m] <= lo) row = m; else rh = m - 1;
+        }
 
-    // ---- cursors over the unit's tiles: (row, tile of the row, tiles and keys of the row) ----
-    struct Cursor { int32_t row, j, n, k; };
-    auto open_row = [&](Cursor& q, int32_t row) {          // the first row from `row` on that this unit works on and whose set is not empty
-        if constexpr (SPLIT) {
-            while (row < a.rows && budget[row] == 0) ++row;
-            q.row = row;
-            q.k = row < a.rows ? budget[row] : 0;
-        } else {
-            q.k = 0;
-            while (row < a.rows && (q.k = budget_of(row)) == 0) {
-                // (an empty set: this unit's warp writes its heads' zeros)
-                for (int i = lane; i < G * DH / 8; i += 32)
-                    reinterpret_cast<uint4*>(a.out + ((int64_t)row * a.n_h + h * G) * DH)[i] = make_uint4(0u, 0u, 0u, 0u);
-                row += units;
+        // ---- addresses of the records: a block's indices, then pages ----
+        int32_t look_row = row;            // (of this lane's last key)
+        int32_t raw[STEPS], raw_row[STEPS], page[STEPS], pos[STEPS];
+        auto key_of = [&](int step) { return h * KPW + step * 32 + lane; };          // in the block
+        auto load_indices = [&](int block) {
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st) {
+                raw_row[st] = -1;
+                const int t = block * BT + key_of(st) / kTile;                         // tile of the run
+                if ((KPW < 32 && lane >= KPW) || t >= n) continue;
+                const int32_t g = lo + t;
+                while (cum[look_row + 1] <= g) ++look_row;
+                const int j = (g - cum[look_row]) * kTile + (lane & (kTile - 1));
+                // places behind the set's end read the tile's first key again (their probabilities are 0)
+                raw[st] = __ldg(a.idx + (int64_t)look_row * a.k_max + (j < budget[look_row] ? j : j & ~(kTile - 1)));
+                raw_row[st] = look_row;
             }
-            q.row = row;
-        }
-        q.n = (q.k + kTile - 1) / kTile;
-        q.j = 0;
-    };
-    auto advance = [&](Cursor& q) { if (++q.j >= q.n) open_row(q, q.row + (SPLIT ? 1 : units)); };
-    Cursor ahead{};                        // the tile whose indices are read next
-    int32_t left = 0;                      // SPLIT: tiles that `ahead` has still to hand out
-    if constexpr (SPLIT) {
-        if (works) {
-            int32_t rl = 0, rh = a.rows - 1;       // the row that holds tile lo (of rows that start there the last: the others are empty)
-            while (rl < rh) {
-                const int32_t m = (rl + rh + 1) >> 1;
-                if (cum[m] <= lo) rl = m; else rh = m - 1;
+        };
+        auto load_pages = [&]() {
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st) {
+                page[st] = -1;
+                if (raw_row[st] < 0) continue;
+                const int32_t b = (a.row0 + raw_row[st]) / a.Lq, len = checked_len(c, b, a.Lk, bad);
+                pos[st] = raw[st];
+                if ((uint32_t)pos[st] >= (uint32_t)len) {
+                    bad = true;
+                    pos[st] = min(max(pos[st], 0), max(len - 1, 0));
+                }
+                page[st] = checked_page(c, b, pos[st], bad);
             }
-            ahead.row = rl; ahead.k = budget[rl]; ahead.n = (ahead.k + kTile - 1) / kTile; ahead.j = lo - cum[rl];
-            left = hi - lo;
-        }
-    } else {
-        open_row(ahead, unit);
-    }
-    Cursor cur = ahead;
+        };
+        auto put_addresses = [&](int slot) {
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st)
+                if (page[st] >= 0)
+                    addresses[slot * (BT * kTile) + key_of(st)] = (int64_t)page[st] * c.page_bytes + (int64_t)(pos[st] & (c.T - 1)) * c.rec;
+        };
+        auto unit_sync = [&]() {
+            if constexpr (NKV == 1) __syncwarp();
+            else asm volatile("bar.sync %0, %1;" ::"r"(1 + sub), "r"(NKV * 32) : "memory");
+        };
+        const int ckey = lane / CPK, cpiece = lane % CPK;
+        const unsigned char* const from_codes = c.pool + h * (DH / 2) + cpiece * 16;
+        const unsigned char* const from_scales = c.pool + D + h * (DH / 8);
+        const uint32_t to_k = ring + ckey * St::kRow + cpiece * 16, to_v = ring + St::kV + ckey * St::kVRow + cpiece * 16;
+        const uint32_t to_s = ring + St::kS + (lane & 15) * St::kSRow;
+        // tile t of the run, whose addresses start at `from`, into stage `off`
+        auto issue = [&](bool real, const int64_t* from, uint32_t off) {
+            if (real) {
+#pragma unroll
+                for (int i = 0; i < kTile / KPI; ++i) {
+                    const unsigned char* src = from_codes + from[ckey + i * KPI];
+                    cp_async16(to_k + off + i * KPI * St::kRow, src);
+                    cp_async16(to_v + off + i * KPI * St::kVRow, src + D / 2);
+                }
+                if (lane < kTile) copy_async<St::kSRow>(to_s + off, from_scales + from[lane]);
+            }
+            cp_async_commit();             // (one group a tile, possibly empty)
+        };
 
-    // ---- what is in flight: indices (lane & 15), then pages, then records ----
-    struct Pos { int32_t raw, n, b, len; };                // n: keys of the tile, 0: no tile
-    struct Token { int32_t page, pos, n; };
-    int32_t row_b = 0, row_len = 0, row_seen = -1;
-    auto next_indices = [&]() -> Pos {
-        Pos f{0, 0, 0, 0};
-        if (SPLIT ? left <= 0 : ahead.row >= a.rows) return f;
-        if (ahead.row != row_seen) {
-            row_seen = ahead.row;
-            row_b = ahead.row / a.Lq;
-            row_len = checked_len(c, row_b, a.Lk, bad);
+        load_indices(0);
+        load_pages();
+        put_addresses(0);
+        if (n > BT) {
+            load_indices(1);
+            load_pages();
+            put_addresses(1);
         }
-        f.b = row_b; f.len = row_len;
-        f.n = min(kTile, ahead.k - ahead.j * kTile);
-        const int j = lane & 15;
-        if (j < f.n) f.raw = __ldg(a.idx + (int64_t)ahead.row * a.k_max + ahead.j * kTile + j);
-        --left;
-        advance(ahead);
-        return f;
-    };
-    auto find_pages = [&](const Pos& f) -> Token {
-        Token t{0, 0, f.n};
-        if (f.n == 0) return t;
-        const int32_t first = __shfl_sync(0xFFFFFFFFu, f.raw, 0);
-        t.pos = (lane & 15) < f.n ? f.raw : first;         // places behind the set's end read one of its keys again (P = 0 there)
-        if ((uint32_t)t.pos >= (uint32_t)f.len) {
-            bad = true;
-            t.pos = min(max(t.pos, 0), max(f.len - 1, 0));
-        }
-        t.page = checked_page(c, f.b, t.pos, bad);
-        return t;
-    };
-    const int D = n_kv * DH;
-    const int ckey = lane / CPK, cpiece = lane % CPK;
-    const unsigned char* const from_codes = c.pool + h * (DH / 2) + cpiece * 16;
-    const unsigned char* const from_scales = c.pool + D + h * (DH / 8);
-    const uint32_t to_k = ring + ckey * St::kRow + cpiece * 16, to_v = ring + St::kV + ckey * St::kVRow + cpiece * 16;
-    const uint32_t to_s = ring + St::kS + (lane & 15) * St::kSRow;
-    int32_t issued = 0;
-    auto issue = [&](const Token& t, uint32_t stage) {
-        if (t.n) {
-            const int64_t at = (int64_t)t.page * c.page_bytes + (int64_t)(t.pos & (c.T - 1)) * c.rec;
-            const uint32_t off = stage * St::kBytes;
+        unit_sync();
+        int next = 0;                      // tile in the address ring (BT tiles a block) of the next one to copy
+        uint32_t next_off = 0;             // its stage
+        auto issue_next = [&](bool real) {
+            issue(real, addresses + next * kTile, next_off);
+            next = next + 1 == kAddressBlocks * BT ? 0 : next + 1;
+            next_off = next_off == (kStages - 1) * St::kBytes ? 0u : next_off + St::kBytes;
+        };
 #pragma unroll
-            for (int i = 0; i < kTile / KPI; ++i) {
-                const int64_t key_at = __shfl_sync(0xFFFFFFFFu, at, ckey + i * KPI);
-                cp_async16(to_k + off + i * KPI * St::kRow, from_codes + key_at);
-                cp_async16(to_v + off + i * KPI * St::kVRow, from_codes + key_at + D / 2);
-            }
-            if (lane < kTile) copy_async<St::kSRow>(to_s + off, from_scales + at);
-            ++issued;
-        }
-        cp_async_commit();                 // (one group a tile, possibly empty)
-    };
+        for (int t = 0; t + 1 < kStages; ++t) issue_next(t < n);
 
-    Pos ahead_pos;
-    Token ahead_token;
-    {
-        Pos f[kStages];
+        uint32_t qf[KW][4];                // Q as the B operand
+        float q_start[SETS][KS][2];        // COLS: what the accumulators start from, -8 times the group's sum of Q
+        float q_scale = a.scale_log2;
+        float o[MT][4], m_run[2], l_run[2];
+        int32_t row_first = cum[row], row_end = cum[row + 1], row_k = budget[row];
+        bool fresh = true;
+        uint32_t st_off = 0;
+        int slot = 1, in_block = 0, block = 0;                 // block's last written slot of addresses, tile in the block
+        for (int32_t i = 0; i < n; ++i) {
+            if (fresh) {
+                fresh = false;
+                const bool mine = COLS ? (G == 4 ? true : (gid >> 1) == tig && (gid & 1) < G) : true;
+                const int head = COLS ? (G == 4 ? gid & 3 : (gid & 1)) : gid;
+                const __nv_bfloat16* qp = a.Q + ((int64_t)row * a.n_h + h * G + (mine ? head : 0)) * DH + tig * (DH / 4);
+                uint4 q[KW];
 #pragma unroll
-        for (int i = 0; i < kStages; ++i) f[i] = works ? next_indices() : Pos{0, 0, 0, 0};
-        Token t[kStages];
+                for (int w = 0; w < KW; ++w) q[w] = mine ? __ldg(reinterpret_cast<const uint4*>(qp) + w) : make_uint4(0u, 0u, 0u, 0u);
+                if constexpr (!COLS) {
 #pragma unroll
-        for (int i = 0; i < kStages; ++i) t[i] = find_pages(f[i]);
-        ahead_pos = works ? next_indices() : Pos{0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i + 1 < kStages; ++i) issue(t[i], i);
-        ahead_token = t[kStages - 1];
-    }
-
-    uint32_t qf[KW][4];
-    float o[MT][4], m_run[2], l_run[2];
-    bool fresh = true;
-    for (int32_t i = 0; i < issued; ++i) {
-        if (fresh) {
-            fresh = false;
-            const bool real = gid < G;
-            const __nv_bfloat16* qp = a.Q + ((int64_t)cur.row * a.n_h + h * G + (real ? gid : 0)) * DH + tig * (DH / 4);
-#pragma unroll
-            for (int w = 0; w < KW; ++w) {
-                const uint4 q = real ? __ldg(reinterpret_cast<const uint4*>(qp) + w) : make_uint4(0u, 0u, 0u, 0u);
-                qf[w][0] = __byte_perm(q.x, q.z, 0x5410); qf[w][1] = __byte_perm(q.x, q.z, 0x7632);
-                qf[w][2] = __byte_perm(q.y, q.w, 0x5410); qf[w][3] = __byte_perm(q.y, q.w, 0x7632);
-            }
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) o[mt][0] = o[mt][1] = o[mt][2] = o[mt][3] = 0.f;
-            m_run[0] = m_run[1] = -INFINITY;
-            l_run[0] = l_run[1] = 0.f;
-        }
-        cp_async_wait<kStages - 2>();      // this tile's records have landed
-        __syncwarp();                      // (everybody's, and the stage of the tile before has been read)
-        issue(ahead_token, (uint32_t)(i + kStages - 1) % kStages);
-        ahead_token = find_pages(ahead_pos);
-        ahead_pos = next_indices();
-        const uint32_t st = ring + (uint32_t)i % kStages * St::kBytes;
-
-        // ---- S^T = K Q^T ----
-        float s[4] = {0.f, 0.f, 0.f, 0.f}, s2[4] = {0.f, 0.f, 0.f, 0.f};
-        {
-            uint32_t kc[2][KW], ks[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                lds_words<KW>(kc[e], st + (gid + 8 * e) * St::kRow + tig * (KW * 4));
-                ks[e] = lds_small<KS>(st + St::kS + (gid + 8 * e) * St::kSRow + tig * KS);
-            }
-#pragma unroll
-            for (int gr = 0; gr < KS; ++gr) {
-                const uint32_t sa = scale_bf16x2((ks[0] >> (8 * gr)) & 255u), sb = scale_bf16x2((ks[1] >> (8 * gr)) & 255u);
-                const uint32_t za = zero_bf16x2(sa), zb = zero_bf16x2(sb);
-#pragma unroll
-                for (int w = gr * (KW / KS); w < (gr + 1) * (KW / KS); ++w) {
-                    uint32_t pa[4], pb[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        pa[j] = fma_bf16x2(code_pair(kc[0][w], j), sa, za);
-                        pb[j] = fma_bf16x2(code_pair(kc[1][w], j), sb, zb);
+                    for (int w = 0; w < KW; ++w) {
+                        qf[w][0] = __byte_perm(q[w].x, q[w].z, 0x5410); qf[w][1] = __byte_perm(q[w].x, q[w].z, 0x7632);
+                        qf[w][2] = __byte_perm(q[w].y, q[w].w, 0x5410); qf[w][3] = __byte_perm(q[w].y, q[w].w, 0x7632);
                     }
-                    mma_bf16_16816(s, pa[0], pb[0], pa[1], pb[1], qf[w][0], qf[w][1]);
-                    mma_bf16_16816(s2, pa[2], pb[2], pa[3], pb[3], qf[w][2], qf[w][3]);
+                } else {
+                    // the exponent of the warp's largest finite |q|
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int w = 0; w < KW; ++w) {
+                        const uint32_t x[4] = {q[w].x, q[w].y, q[w].z, q[w].w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t lo_e = (x[e] >> 7) & 255u, hi_e = (x[e] >> 23) & 255u;
+                            top = max(top, max(lo_e == 255u ? 0u : lo_e, hi_e == 255u ? 0u : hi_e));
+                        }
+                    }
+                    top = max(__reduce_max_sync(0xFFFFFFFFu, top), 20u);
+                    const float up = __uint_as_float((127u + 14u + 127u - top) << 23);
+                    q_scale = a.scale_log2 * 16777216.0f / up;                         // (2^24: what a code's place is worth)
+                    float sum[KS];
+#pragma unroll
+                    for (int gr = 0; gr < KS; ++gr) sum[gr] = 0.f;
+#pragma unroll
+                    for (int w = 0; w < KW; ++w) {
+                        float f[8];
+                        const uint32_t x[4] = {q[w].x, q[w].y, q[w].z, q[w].w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            f[2 * e] = __uint_as_float(x[e] << 16) * up;
+                            f[2 * e + 1] = __uint_as_float(x[e] & 0xFFFF0000u) * up;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sum[w / (KW / KS)] += f[e];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) qf[w][e] = (e & 1) ? pack_f16(f[e] * 0.0625f, f[e + 4] * 0.0625f) : pack_f16(f[e], f[e + 4]);
+                    }
+                    // this lane's columns: slot tig, heads 0 and 1; with four heads slot 2 set + (tig >> 1), heads 2 (tig & 1), + 1
+#pragma unroll
+                    for (int set = 0; set < SETS; ++set)
+#pragma unroll
+                        for (int gr = 0; gr < KS; ++gr)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int from_slot = G == 4 ? 2 * set + (tig >> 1) : tig;
+                                const int from_gid = G == 4 ? 2 * (tig & 1) + e : 2 * tig + e;
+                                q_start[set][gr][e] = -8.0f / 16777216.0f * __shfl_sync(0xFFFFFFFFu, sum[gr], from_gid * 4 + from_slot);
+                            }
+                }
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) o[mt][0] = o[mt][1] = o[mt][2] = o[mt][3] = 0.f;
+                m_run[0] = m_run[1] = -INFINITY;
+                l_run[0] = l_run[1] = 0.f;
+            }
+            // ---- addresses ahead ----
+            if (in_block == 0) {
+                if (block >= 1 && (block + 1) * BT < n) {
+                    slot = slot + 1 == kAddressBlocks ? 0 : slot + 1;
+                    put_addresses(slot);
+                    unit_sync();
+                }
+                if ((block + 2) * BT < n) load_indices(block + 2);
+            } else if (in_block == BT / 2) {
+                if ((block + 2) * BT < n) load_pages();
+            }
+            if (++in_block == BT) { in_block = 0; ++block; }
+            cp_async_wait<kStages - 2>();  // this tile's records have landed
+            __syncwarp();                  // (everybody's, and the stage of the tile before has been read)
+            issue_next(i + kStages - 1 < n);
+            const uint32_t st = ring + st_off;
+            st_off = st_off == (kStages - 1) * St::kBytes ? 0u : st_off + St::kBytes;
+
+            // ---- S^T = K Q^T ----
+            float s[4];
+            {
+                uint32_t kc[2][KW];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) lds_words<KW>(kc[e], st + (gid + 8 * e) * St::kRow + tig * (KW * 4));
+                if constexpr (COLS) {
+                    float acc[SETS][KS][4];
+#pragma unroll
+                    for (int set = 0; set < SETS; ++set)
+#pragma unroll
+                        for (int gr = 0; gr < KS; ++gr)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[set][gr][e] = q_start[set][gr][e & 1];
+#pragma unroll
+                    for (int w = 0; w < KW; ++w) {
+                        uint32_t x[2][4];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t v = kc[e][w], v8 = v >> 8;
+                            x[e][0] = v & 0x000F000Fu; x[e][1] = v & 0x00F000F0u;
+                            x[e][2] = v8 & 0x000F000Fu; x[e][3] = v8 & 0x00F000F0u;
+                        }
+#pragma unroll
+                        for (int set = 0; set < SETS; ++set) {
+                            const bool on = G != 4 || 2 * set + (gid >> 2) == tig;     // four heads: Q of a set's two slots
+                            float(&ac)[4] = acc[set][w / (KW / KS)];
+                            mma_f16_16816(ac, x[0][0], x[1][0], x[0][1], x[1][1], on ? qf[w][0] : 0u, on ? qf[w][1] : 0u);
+                            mma_f16_16816(ac, x[0][2], x[1][2], x[0][3], x[1][3], on ? qf[w][2] : 0u, on ? qf[w][3] : 0u);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[e] = 0.f;
+#pragma unroll
+                    for (int set = 0; set < SETS; ++set) {
+                        const int sl = G == 4 ? 2 * set + (tig >> 1) : tig;
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t ks = lds_small<KS>(st + St::kS + (gid + 8 * e) * St::kSRow + sl * KS);
+#pragma unroll
+                            for (int gr = 0; gr < KS; ++gr) {
+                                const float f = scale_f32((ks >> (8 * gr)) & 255u);
+                                s[2 * e] = fmaf(acc[set][gr][2 * e], f, s[2 * e]);
+                                s[2 * e + 1] = fmaf(acc[set][gr][2 * e + 1], f, s[2 * e + 1]);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (G != 4) s[e] += __shfl_xor_sync(0xFFFFFFFFu, s[e], 1);
+                        s[e] += __shfl_xor_sync(0xFFFFFFFFu, s[e], 2);
+                    }
+                } else {
+                    float s2[4] = {0.f, 0.f, 0.f, 0.f};
+                    uint32_t ks[2];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[e] = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) ks[e] = lds_small<KS>(st + St::kS + (gid + 8 * e) * St::kSRow + tig * KS);
+#pragma unroll
+                    for (int gr = 0; gr < KS; ++gr) {
+                        const uint32_t sa = scale_bf16x2((ks[0] >> (8 * gr)) & 255u), sb = scale_bf16x2((ks[1] >> (8 * gr)) & 255u);
+                        const uint32_t za = zero_bf16x2(sa), zb = zero_bf16x2(sb);
+#pragma unroll
+                        for (int w = gr * (KW / KS); w < (gr + 1) * (KW / KS); ++w) {
+                            uint32_t pa[4], pb[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                pa[j] = fma_bf16x2(code_pair(kc[0][w], j), sa, za);
+                                pb[j] = fma_bf16x2(code_pair(kc[1][w], j), sb, zb);
+                            }
+                            mma_bf16_16816(s, pa[0], pb[0], pa[1], pb[1], qf[w][0], qf[w][1]);
+                            mma_bf16_16816(s2, pa[2], pb[2], pa[3], pb[3], qf[w][2], qf[w][3]);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[e] += s2[e];
                 }
             }
-        }
 
-        // ---- softmax against a reference that few scores move ----
-        const int j0 = cur.j * kTile + gid;
-        const bool v0 = j0 < cur.k, v1 = j0 + 8 < cur.k;
-        float sc[4];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            sc[e] = v0 ? (s[e] + s2[e]) * a.scale_log2 : -INFINITY;
-            sc[2 + e] = v1 ? (s[2 + e] + s2[2 + e]) * a.scale_log2 : -INFINITY;
-        }
-        const bool jump = fmaxf(sc[0], sc[2]) > m_run[0] + kRefSlack || fmaxf(sc[1], sc[3]) > m_run[1] + kRefSlack;
-        if (__any_sync(0xFFFFFFFFu, jump)) {
-            float alpha[2];
+            // ---- softmax against a reference that few scores move ----
+            const int left = row_k - (lo + i - row_first) * kTile;             // keys of this tile, if below 16
+            float sc[4];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float mx = fmaxf(sc[e], sc[2 + e]);
-                mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
-                mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
-                mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
-                const float m_new = fmaxf(m_run[e], mx - kRefUnder);
-                alpha[e] = ex2(m_run[e] - m_new);
-                m_run[e] = m_new;
-                l_run[e] *= alpha[e];
+                sc[e] = gid < left ? s[e] * q_scale : -INFINITY;
+                sc[2 + e] = gid + 8 < left ? s[2 + e] * q_scale : -INFINITY;
             }
+            const bool jump = fmaxf(sc[0], sc[2]) > m_run[0] + kRefSlack || fmaxf(sc[1], sc[3]) > m_run[1] + kRefSlack;
+            if (__any_sync(0xFFFFFFFFu, jump)) {
+                float alpha[2];
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                o[mt][0] *= alpha[0]; o[mt][1] *= alpha[1]; o[mt][2] *= alpha[0]; o[mt][3] *= alpha[1];
-            }
-        }
-        float p[4];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            p[e] = ex2(sc[e] - m_run[e]);
-            p[2 + e] = ex2(sc[2 + e] - m_run[e]);
-            l_run[e] += p[e] + p[2 + e];
-        }
-        const uint32_t pb0 = transposed(pack_f16(p[0], p[1])), pb1 = transposed(pack_f16(p[2], p[3]));
-
-        // ---- O^T += V'^T P^T ----
-        {
-            uint32_t vc[4][VW];
-            float vs[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int key = 2 * tig + (e & 1) + 8 * (e >> 1);
-                lds_words<VW>(vc[e], st + St::kV + key * St::kVRow + gid * (VW * 4));
-                vs[e] = scale_f32(lds_small<1>(st + St::kS + key * St::kSRow + DH / 16 + (DH == 128 ? gid : gid >> 1)));
-            }
-            const uint32_t sa = pack_f16(vs[0], vs[1]), sb = pack_f16(vs[2], vs[3]);
-#pragma unroll
-            for (int w = 0; w < VW; ++w)
-#pragma unroll
-                for (int hf = 0; hf < 2; ++hf) {
-                    uint32_t va[4], vb[4];
-                    values_f16x2(va, __byte_perm(vc[0][w], vc[1][w], hf ? 0x7632 : 0x5410), sa);
-                    values_f16x2(vb, __byte_perm(vc[2][w], vc[3][w], hf ? 0x7632 : 0x5410), sb);
-                    mma_f16_16816(o[w * 4 + hf * 2], va[0], va[1], vb[0], vb[1], pb0, pb1);
-                    mma_f16_16816(o[w * 4 + hf * 2 + 1], va[2], va[3], vb[2], vb[3], pb0, pb1);
+                for (int e = 0; e < 2; ++e) {
+                    float mx = fmaxf(sc[e], sc[2 + e]);
+                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
+                    const float m_new = fmaxf(m_run[e], mx - kRefUnder);
+                    alpha[e] = ex2(m_run[e] - m_new);
+                    m_run[e] = m_new;
+                    l_run[e] *= alpha[e];
                 }
-        }
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    o[mt][0] *= alpha[0]; o[mt][1] *= alpha[1]; o[mt][2] *= alpha[0]; o[mt][3] *= alpha[1];
+                }
+            }
+            float p[4];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                p[e] = ex2(sc[e] - m_run[e]);
+                p[2 + e] = ex2(sc[2 + e] - m_run[e]);
+                l_run[e] += p[e] + p[2 + e];
+            }
+            // (with groups in columns every lane of a key has its scores; the columns of P are those of the heads that there are)
+            const bool head_cols = !COLS || 2 * tig < G;
+            const uint32_t pb0 = transposed(head_cols ? pack_f16(p[0], p[1]) : 0u), pb1 = transposed(head_cols ? pack_f16(p[2], p[3]) : 0u);
 
-        // ---- end of the row, or of this unit's part of it ----
-        const bool last = i + 1 >= issued;
-        if (cur.j + 1 >= cur.n || last) {
-            float l[2];
+            // ---- O^T += V'^T P^T ----
+            {
+                uint32_t vc[4][VW];
+                float vs[4];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                l[e] = l_run[e];
-                l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 4);
-                l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 8);
-                l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 16);
+                for (int e = 0; e < 4; ++e) {
+                    const int key = 2 * tig + (e & 1) + 8 * (e >> 1);
+                    lds_words<VW>(vc[e], st + St::kV + key * St::kVRow + gid * (VW * 4));
+                    vs[e] = scale_f32(lds_small<1>(st + St::kS + key * St::kSRow + DH / 16 + (DH == 128 ? gid : gid >> 1)));
+                }
+                const uint32_t sa = pack_f16(vs[0], vs[1]), sb = pack_f16(vs[2], vs[3]);
+#pragma unroll
+                for (int w = 0; w < VW; ++w)
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {
+                        uint32_t va[4], vb[4];
+                        values_f16x2(va, __byte_perm(vc[0][w], vc[1][w], hf ? 0x7632 : 0x5410), sa);
+                        values_f16x2(vb, __byte_perm(vc[2][w], vc[3][w], hf ? 0x7632 : 0x5410), sb);
+                        mma_f16_16816(o[w * 4 + hf * 2], va[0], va[1], vb[0], vb[1], pb0, pb1);
+                        mma_f16_16816(o[w * 4 + hf * 2 + 1], va[2], va[3], vb[2], vb[3], pb0, pb1);
+                    }
             }
-            bool whole = true;
-            int32_t slot = 0;
-            if constexpr (SPLIT) {
-                whole = cum[cur.row] >= lo && cum[cur.row + 1] <= hi;
-                slot = 2 * unit + (cum[cur.row] > lo ? 1 : 0);
-            }
+
+            // ---- end of the row, or of this unit's part of it ----
+            if (lo + i + 1 == row_end || i + 1 == n) {
+                float l[2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int head = 2 * tig + e;
-                if (head < G) {
-                    float v[DL];
+                for (int e = 0; e < 2; ++e) {
+                    l[e] = l_run[e];
+                    l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 4);
+                    l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 8);
+                    l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 16);
+                }
+                const bool whole = row_first >= lo && row_end <= lo + n;
+                const int32_t part = 2 * unit + (row_first > lo ? 1 : 0);
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) { v[2 * mt] = o[mt][e]; v[2 * mt + 1] = o[mt][2 + e]; }
-                    if (whole) {
-                        const float inv = 1.0f / l[e];
+                for (int e = 0; e < 2; ++e) {
+                    const int head = 2 * tig + e;
+                    if (head < G) {
+                        float v[DL];
 #pragma unroll
-                        for (int d = 0; d < DL; ++d) v[d] *= inv;
-                        write_gated<DL>(a, ((int64_t)cur.row * a.n_h + h * G + head) * DH + gid * DL, v);
-                    } else {
-                        const int64_t sh = (int64_t)slot * a.n_h + h * G + head;
-                        float4* to = reinterpret_cast<float4*>(a.state + sh * DH + gid * DL);
+                        for (int mt = 0; mt < MT; ++mt) { v[2 * mt] = o[mt][e]; v[2 * mt + 1] = o[mt][2 + e]; }
+                        if (whole) {
+                            const float inv = 1.0f / l[e];
 #pragma unroll
-                        for (int d = 0; d < DL / 4; ++d) to[d] = make_float4(v[4 * d], v[4 * d + 1], v[4 * d + 2], v[4 * d + 3]);
-                        if (gid == 0) a.stats[sh] = make_float2(m_run[e], l[e]);
+                            for (int d = 0; d < DL; ++d) v[d] *= inv;
+                            write_gated<DL>(a, ((int64_t)row * a.n_h + h * G + head) * DH + gid * DL, v);
+                        } else {
+                            const int64_t sh = (int64_t)part * a.n_h + h * G + head;
+                            float4* to = reinterpret_cast<float4*>(a.state + sh * DH + gid * DL);
+#pragma unroll
+                            for (int d = 0; d < DL / 4; ++d) to[d] = make_float4(v[4 * d], v[4 * d + 1], v[4 * d + 2], v[4 * d + 3]);
+                            if (gid == 0) a.stats[sh] = make_float2(m_run[e], l[e]);
+                        }
                     }
                 }
+                fresh = true;
+                if (i + 1 < n) {
+                    do ++row; while (cum[row + 1] <= row_end);             // (rows with an empty set are passed over)
+                    row_first = row_end; row_end = cum[row + 1]; row_k = budget[row];
+                }
             }
-            fresh = true;
         }
-        if (!last) advance(cur);
     }
-    if constexpr (SPLIT) {
-        // what the merge needs, and rows with an empty set
-        if (blockIdx.x == 0)
-            for (int r = threadIdx.x; r <= a.rows; r += kWarps * 32) a.cum[r] = cum[r];
-        const int64_t row_vec = (int64_t)a.n_h * DH / 8;
-        for (int r = blockIdx.x; r < a.rows; r += gridDim.x)
-            if (budget[r] == 0)
-                for (int i = threadIdx.x; i < row_vec; i += kWarps * 32) reinterpret_cast<uint4*>(a.out)[r * row_vec + i] = make_uint4(0u, 0u, 0u, 0u);
-    }
+    // what the merge needs, and rows with an empty set
+    if (blockIdx.x == 0)
+        for (int r = threadIdx.x; r <= a.rows; r += kWarps * 32) a.cum[r] = cum[r];
+    const int64_t row_vec = (int64_t)a.n_h * DH / 8;
+    for (int r = blockIdx.x; r < a.rows; r += gridDim.x)
+        if (budget[r] == 0)
+            for (int i = threadIdx.x; i < row_vec; i += kWarps * 32) reinterpret_cast<uint4*>(a.out)[r * row_vec + i] = make_uint4(0u, 0u, 0u, 0u);
     if (bad) cta_bad = 1;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        if constexpr (SPLIT) a.flags[blockIdx.x] = cta_bad;
-        else if (cta_bad) report_bad_index(a.status);
-    }
+    if (threadIdx.x == 0) a.flags[blockIdx.x] = cta_bad;
 }
 
 // Rows whose parts lie in several units' runs: the parts' states in their order, normalised, gated, rounded.  WPI warps share a
@@ -543,7 +642,8 @@ __global__ void __launch_bounds__(kMergeWarps * 32) gsa_cache_merge_kernel(const
         int bad = 0;
         for (int i = threadIdx.x; i < ctas; i += kMergeWarps * 32) bad |= a.flags[i];
         bad = __syncthreads_or(bad);
-        if (threadIdx.x < kStatusBytes / 4) a.status[threadIdx.x] = threadIdx.x == 0 && bad ? kDevBadIndex : kDevOk;
+        if (threadIdx.x < kStatusBytes / 4)                // (a call's later launches add to what its first one found)
+            a.status[threadIdx.x] = threadIdx.x == 0 && (bad || (a.row0 && a.status[0])) ? kDevBadIndex : kDevOk;
         return;
     }
     __shared__ float part_o[WPI > 1 ? WPI : 1][DH];
@@ -646,16 +746,35 @@ __global__ void __launch_bounds__(kMergeWarps * 32) gsa_cache_merge_kernel(const
 
 int32_t unit_count(const gsa_params_t& p) { return sm_count() * kCtasPerSm * (kWarps / p.n_kv); }
 
-template <int DH, int G, bool SPLIT>
+template <int DH, int G, int NKV>
 cudaError_t launch_main(const CacheAttnArgs& a, cudaStream_t st) {
-    const int subs = kWarps / a.c.n_kv;
-    const size_t smem = (SPLIT ? row_table_bytes(a.rows) : 0) + (size_t)kWarps * kStages * Stage<DH>::kBytes;
-    // (set on every call: the attribute belongs to the current device)
-    cudaError_t e = cudaFuncSetAttribute(gsa_cache_attn_kernel<DH, G, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static std::atomic<uint64_t> granted{0};
+    constexpr size_t fixed = fixed_smem<DH, NKV>();
+    cudaError_t e = grant_smem(granted, reinterpret_cast<const void*>(gsa_cache_attn_kernel<DH, G, NKV>), fixed + row_table_bytes(kMaxSplitRows));
     if (e != cudaSuccess) return e;
-    e = launch_chained(gsa_cache_attn_kernel<DH, G, SPLIT>, (unsigned)(a.units / subs), kWarps * 32, smem, st, a);
+    e = launch_chained(gsa_cache_attn_kernel<DH, G, NKV>, (unsigned)(a.units / (kWarps / NKV)), kWarps * 32, fixed + row_table_bytes(a.rows), st, a);
     ++g_launches;
     return e != cudaSuccess ? e : cudaGetLastError();
+}
+template <int DH, int G>
+cudaError_t launch_heads(const CacheAttnArgs& a, cudaStream_t st) {
+    switch (a.c.n_kv) {
+        case 1: return launch_main<DH, G, 1>(a, st);
+        case 2: return launch_main<DH, G, 2>(a, st);
+        case 4: return launch_main<DH, G, 4>(a, st);
+        case 8: return launch_main<DH, G, 8>(a, st);
+    }
+    return cudaErrorInvalidValue;
+}
+template <int DH>
+cudaError_t launch_groups(const CacheAttnArgs& a, cudaStream_t st) {
+    switch (a.n_h / a.c.n_kv) {
+        case 1: return launch_heads<DH, 1>(a, st);
+        case 2: return launch_heads<DH, 2>(a, st);
+        case 4: return launch_heads<DH, 4>(a, st);
+        case 8: return launch_heads<DH, 8>(a, st);
+    }
+    return cudaErrorInvalidValue;
 }
 
 template <int DH, int WPI>
@@ -668,55 +787,46 @@ cudaError_t launch_merge(const CacheAttnArgs& a, int32_t by_cut, int32_t items, 
 
 struct Plan { size_t stats, cum, flags, total; };
 Plan plan_scratch(const gsa_params_t& p) {
-    const size_t slots = 2 * (size_t)unit_count(p), rows = (size_t)p.B * p.Lq;
+    const size_t slots = 2 * (size_t)unit_count(p);
+    const int64_t all = (int64_t)p.B * p.Lq, rows = all < kMaxSplitRows ? all : kMaxSplitRows;
     Plan w;
     w.stats = align_up(slots * p.n_h * p.d_h * 4, 256);
     w.cum = w.stats + align_up(slots * p.n_h * 8, 256);
-    w.flags = w.cum + align_up((rows + 1) * 4, 256);
+    w.flags = w.cum + align_up((size_t)(rows + 1) * 4, 256);
     w.total = w.flags + align_up((size_t)sm_count() * kCtasPerSm * 4, 256);
     return w;
 }
 
 }  // namespace
 
-size_t cache_attn_scratch_bytes(const gsa_params_t& p) {
-    return (int64_t)p.B * p.Lq > kMaxSplitRows ? 0 : plan_scratch(p).total;
-}
+size_t cache_attn_scratch_bytes(const gsa_params_t& p) { return plan_scratch(p).total; }
 
 cudaError_t launch_cache_attn(const CacheView& c, const gsa_params_t& p, const __nv_bfloat16* Q, const __nv_bfloat16* g1,
                               const int32_t* idx, const int32_t* kt, __nv_bfloat16* out, int32_t* ws, cudaStream_t st) {
     CacheAttnArgs a{};
-    a.c = c; a.Q = Q; a.g1 = g1; a.idx = idx; a.kt = kt; a.out = out;
-    a.rows = p.B * p.Lq; a.Lq = p.Lq; a.Lk = p.Lk; a.n_h = p.n_h; a.k_max = p.k_max;
+    a.c = c; a.Lq = p.Lq; a.Lk = p.Lk; a.n_h = p.n_h; a.k_max = p.k_max;
     a.scale_log2 = (p.sm_scale > 0.f ? p.sm_scale : 1.0f / sqrtf((float)p.d_h)) * 1.4426950408889634f;
-    a.status = ws;
-    const bool split = a.rows <= kMaxSplitRows;
-    const int subs = kWarps / p.n_kv;
-    a.units = unit_count(p);
-    cudaError_t e = cudaSuccess;
-    if (split) {
-        const Plan w = plan_scratch(p);
-        char* s = (char*)ws + kStatusBytes;
-        a.state = (float*)s; a.stats = (float2*)(s + w.stats); a.cum = (int32_t*)(s + w.cum); a.flags = (int32_t*)(s + w.flags);
+    const Plan w = plan_scratch(p);
+    char* s = (char*)ws + kStatusBytes;
+    a.status = ws; a.state = (float*)s; a.stats = (float2*)(s + w.stats); a.cum = (int32_t*)(s + w.cum); a.flags = (int32_t*)(s + w.flags);
+    const int32_t all = p.B * p.Lq, subs = kWarps / p.n_kv;
+    for (int32_t r0 = 0; r0 < all; r0 += kMaxSplitRows) {
+        const int64_t at = (int64_t)r0 * p.n_h * p.d_h;
+        a.row0 = r0; a.rows = all - r0 < kMaxSplitRows ? all - r0 : kMaxSplitRows;
+        a.Q = Q + at; a.g1 = g1 + at; a.out = out + at; a.idx = idx + (int64_t)r0 * p.k_max; a.kt = kt + r0;
         // no more CTAs than the largest sets would keep busy
-        const int64_t most = units_for((int64_t)a.rows * ((p.k_max + kTile - 1) / kTile), a.units);
+        const int64_t most = units_for((int64_t)a.rows * ((p.k_max + kTile - 1) / kTile), unit_count(p));
         a.units = (int32_t)((most + subs - 1) / subs * subs);
-    } else {
-        e = launch_clear(st, {ws, (size_t)kStatusBytes});  // (with a merge, that writes the head)
+        cudaError_t e = p.d_h == 128 ? launch_groups<128>(a, st) : launch_groups<64>(a, st);
+        if (e != cudaSuccess) return e;
+        const int32_t by_cut = a.rows > a.units - 1 ? 1 : 0;
+        const int32_t items = (by_cut ? a.units - 1 : a.rows) * p.n_h;
+        const bool many = !by_cut && a.units >= 8 * a.rows;        // parts of a row: eight or more
+        if (p.d_h == 128) e = many ? launch_merge<128, 8>(a, by_cut, items, st) : launch_merge<128, 1>(a, by_cut, items, st);
+        else e = many ? launch_merge<64, 8>(a, by_cut, items, st) : launch_merge<64, 1>(a, by_cut, items, st);
+        if (e != cudaSuccess) return e;
     }
-    if (e != cudaSuccess) return e;
-    e = cudaErrorInvalidValue;
-#define GSA_CACHE_CASE(DH_, G_) \
-    if (p.d_h == DH_ && p.n_h / p.n_kv == G_) e = split ? launch_main<DH_, G_, true>(a, st) : launch_main<DH_, G_, false>(a, st)
-    GSA_CACHE_CASE(128, 1); GSA_CACHE_CASE(128, 2); GSA_CACHE_CASE(128, 4); GSA_CACHE_CASE(128, 8);
-    GSA_CACHE_CASE(64, 1); GSA_CACHE_CASE(64, 2); GSA_CACHE_CASE(64, 4); GSA_CACHE_CASE(64, 8);
-#undef GSA_CACHE_CASE
-    if (e != cudaSuccess || !split) return e;
-    const int32_t by_cut = a.rows > a.units - 1 ? 1 : 0;
-    const int32_t items = (by_cut ? a.units - 1 : a.rows) * p.n_h;
-    const bool many = !by_cut && a.units >= 8 * a.rows;    // parts of a row: eight or more
-    if (p.d_h == 128) return many ? launch_merge<128, 8>(a, by_cut, items, st) : launch_merge<128, 1>(a, by_cut, items, st);
-    return many ? launch_merge<64, 8>(a, by_cut, items, st) : launch_merge<64, 1>(a, by_cut, items, st);
+    return cudaSuccess;
 }
 
 }  // namespace gsa

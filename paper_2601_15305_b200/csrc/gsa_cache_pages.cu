@@ -383,13 +383,13 @@ __global__ void __launch_bounds__(256) gsa_cache_release_kernel(const CacheView 
 
 size_t plan_smem(const CacheView& c) { return sizeof(PlanShared) + (size_t)(c.n_pages + 31) / 32 * 4; }
 
-template <class... P, class... A>
-cudaError_t launch_plan(void (*kern)(P...), const CacheView& c, cudaStream_t st, A... args) {
+template <auto KERN, class... A>
+cudaError_t launch_plan(const CacheView& c, cudaStream_t st, A... args) {
+    static std::atomic<uint64_t> granted{0};
     const size_t smem = plan_smem(c);
-    // (set on every call: the attribute belongs to the current device)
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = grant_smem(granted, reinterpret_cast<const void*>(KERN), sizeof(PlanShared) + (1 << 20) / 8);
     if (e != cudaSuccess) return e;
-    launch_chained(kern, 1, kPlanThreads, smem, st, args...);
+    launch_chained(KERN, 1, kPlanThreads, smem, st, args...);
     ++g_launches;
     return cudaGetLastError();
 }
@@ -399,11 +399,11 @@ cudaError_t launch_plan(void (*kern)(P...), const CacheView& c, cudaStream_t st,
 size_t cache_page_list_bytes(const CacheView& c) { return align_up((size_t)c.n_pages * 12, 256); }
 
 cudaError_t launch_cache_reserve(const CacheView& c, const int32_t* n_new, int32_t* start, int32_t* ws, cudaStream_t st) {
-    return launch_plan(gsa_cache_reserve_kernel, c, st, c, n_new, start, ws);
+    return launch_plan<gsa_cache_reserve_kernel>(c, st, c, n_new, start, ws);
 }
 
 cudaError_t launch_cache_fork(const CacheView& c, const int32_t* src_of, bool share, int32_t* ws, cudaStream_t st) {
-    cudaError_t e = launch_plan(gsa_cache_fork_kernel, c, st, c, src_of, share ? 1 : 0, ws);
+    cudaError_t e = launch_plan<gsa_cache_fork_kernel>(c, st, c, src_of, share ? 1 : 0, ws);
     if (e != cudaSuccess) return e;
     launch_chained(gsa_cache_fork_copy_kernel, sm_count() * 4, 256, 0, st, c, src_of, share ? 1 : 0, ws);
     ++g_launches;
@@ -417,7 +417,7 @@ cudaError_t launch_cache_release(const CacheView& c, const int32_t* drop, int32_
 }
 
 cudaError_t launch_cache_compact(const CacheView& c, int32_t* live_pages, int32_t* ws, cudaStream_t st) {
-    cudaError_t e = launch_plan(gsa_cache_compact_kernel, c, st, c, live_pages, ws);
+    cudaError_t e = launch_plan<gsa_cache_compact_kernel>(c, st, c, live_pages, ws);
     if (e != cudaSuccess) return e;
     launch_chained(gsa_cache_compact_copy_kernel, sm_count() * 4, 256, 0, st, c, ws);
     ++g_launches;

@@ -72,6 +72,19 @@ cudaError_t launch_chained(void (*kern)(P...), dim3 grid, dim3 block, size_t sme
     return launch_chained_cluster(1, kern, grid, block, smem, st, static_cast<A&&>(args)...);
 }
 
+// Room for a kernel's dynamic shared memory on the current device.  Asked for once per kernel and device (`granted` is the kernel's own
+// mask of devices, with room for the largest size that it is ever launched with): the runtime's call takes longer than a launch's checks.
+inline cudaError_t grant_smem(std::atomic<uint64_t>& granted, const void* kern, size_t most) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (bit && (granted.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+    if (e == cudaSuccess) granted.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
+
 // Zeroes one or two regions (4-byte aligned, whole words) ahead of a call's kernels.  A kernel of its own, chained like the others:
 // a cudaMemsetAsync stands 2 to 4 us apart from the kernels on either side of it (the three in front of the indexer loss 12 us).
 struct ClearSpan { void* p; size_t bytes; };
