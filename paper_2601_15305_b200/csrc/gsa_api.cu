@@ -3,6 +3,7 @@
 #include <math.h>
 #include <stdio.h>
 
+#include "gsa_cache.cuh"
 #include "gsa_masked.cuh"
 
 namespace gsa {
@@ -690,10 +691,18 @@ int gsa_device_status(const void* ws, void* stream, int32_t* status_out) {
         if (e != cudaSuccess) return cuda_rc(e);
         ws = builtin;
     }
-    int32_t v = 0;
-    cudaError_t e = cudaMemcpyAsync(&v, ws, sizeof(v), cudaMemcpyDeviceToHost, (cudaStream_t)stream);
+    int32_t head[kStatusBytes / 4] = {};
+    cudaError_t e = cudaMemcpyAsync(head, ws, sizeof(head), cudaMemcpyDeviceToHost, (cudaStream_t)stream);
     if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_rc(e);
+    int32_t v = head[0];
+    if (v == kDevOk && head[kFlagsWord] > 0 && head[kFlagsWord] <= kMaxFlags) {      // (words that the call's CTAs wrote, gsa_cache.cuh)
+        int32_t flags[kMaxFlags];
+        e = cudaMemcpyAsync(flags, (const char*)ws + kStatusBytes, (size_t)head[kFlagsWord] * 4, cudaMemcpyDeviceToHost, (cudaStream_t)stream);
+        if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
+        if (e != cudaSuccess) return cuda_rc(e);
+        for (int i = 0; i < head[kFlagsWord] && v == kDevOk; ++i) v = flags[i];
+    }
     if (status_out) *status_out = v;
     return v == kDevOk ? GSA_OK : v == kDevBadIndex ? GSA_ERR_INDEX_RANGE : v == kDevCacheFull ? GSA_ERR_CACHE_FULL : GSA_ERR_DEVICE_TIMEOUT;
 }

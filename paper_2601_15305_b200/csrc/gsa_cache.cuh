@@ -36,19 +36,35 @@ __device__ __forceinline__ int32_t checked_page(const CacheView& c, int32_t b, i
     return 0;
 }
 
+// What the CTAs of a call found wrong.  Each writes a word of its own behind the head, the first one the head, which says how many there are:
+// gsa_device_status adds them up.  Nothing has to be cleared ahead of the call, which would be a launch of its own (2 us of the GPU, as
+// much of the host).  Called by all threads of every CTA of a one-dimensional grid of at most kMaxFlags; launches of one call
+// after its first (`before` != 0) add to the words.
+constexpr int kFlagsWord = 10;             // int32 word of the head: number of words behind it (0: the status word is all there is)
+constexpr int kMaxFlags = 4096;
+__device__ __forceinline__ void write_flags(int32_t* ws, bool bad, int32_t before = 0) {
+    const int any = __syncthreads_or(bad);
+    if (threadIdx.x == 0) {
+        int32_t* mine = ws + kStatusBytes / 4 + blockIdx.x;
+        *mine = (any || (before && *mine)) ? kDevBadIndex : kDevOk;
+    }
+    if (blockIdx.x == 0 && !before)
+        for (int i = threadIdx.x; i < kStatusBytes / 4; i += blockDim.x) ws[i] = i == kFlagsWord ? (int32_t)gridDim.x : 0;
+}
+
 // ---- launchers -------------------------------------------------------------------------------------------------------------
 size_t cache_page_list_bytes(const CacheView& c);        // scratch of the page calls behind the status head
 cudaError_t launch_cache_reserve(const CacheView& c, const int32_t* n_new, int32_t* start, int32_t* ws, cudaStream_t st);
 cudaError_t launch_cache_fork(const CacheView& c, const int32_t* src_of, bool share, int32_t* ws, cudaStream_t st);
-cudaError_t launch_cache_release(const CacheView& c, const int32_t* drop, int32_t* dev_status, cudaStream_t st);
+cudaError_t launch_cache_release(const CacheView& c, const int32_t* drop, int32_t* ws, cudaStream_t st);
 cudaError_t launch_cache_compact(const CacheView& c, int32_t* live_pages, int32_t* ws, cudaStream_t st);
 cudaError_t launch_cache_append(const CacheView& c, int32_t L_new, const __nv_bfloat16* K, const __nv_bfloat16* V,
                                 const __nv_bfloat16* g2, const __nv_bfloat16* kI, const int32_t* n_new, const int32_t* start,
-                                int32_t* dev_status, cudaStream_t st);
+                                int32_t* ws, cudaStream_t st);
 cudaError_t launch_cache_read(const CacheView& c, int32_t L, __nv_bfloat16* K, __nv_bfloat16* V, __nv_bfloat16* kI,
-                              int32_t* dev_status, cudaStream_t st);
-cudaError_t launch_cache_indexer(const CacheView& c, const gsa_params_t& p, RowRange rr, const __nv_bfloat16* qI, const float* w,
-                                 const float* bI, float* scores, int64_t row_stride, int32_t* dev_status, cudaStream_t st);
+                              int32_t* ws, cudaStream_t st);
+cudaError_t launch_cache_indexer(const CacheView& c, const gsa_params_t& p, const __nv_bfloat16* qI, const float* w, const float* bI,
+                                 float* scores, int64_t row_stride, int32_t* ws, cudaStream_t st);
 size_t cache_attn_scratch_bytes(const gsa_params_t& p);
 cudaError_t launch_cache_attn(const CacheView& c, const gsa_params_t& p, const __nv_bfloat16* Q, const __nv_bfloat16* g1,
                               const int32_t* idx, const int32_t* kt, __nv_bfloat16* out, int32_t* ws, cudaStream_t st);

@@ -46,13 +46,12 @@ int check_stage(const gsa_cache_t* c, const gsa_params_t* p, CacheView* v) {
     return GSA_OK;
 }
 
-size_t list_ws_bytes(const CacheView& v) { return kStatusBytes + cache_page_list_bytes(v); }
+size_t list_ws_bytes(const CacheView& v) {
+    const size_t lists = cache_page_list_bytes(v), flags = kMaxFlags * 4;
+    return kStatusBytes + (lists > flags ? lists : flags);
+}
 
 bool ws_ok(const void* ws, size_t have, size_t need) { return ws && aligned16(ws) && have >= need; }
-
-int clear_status(void* ws, void* stream) {
-    return cuda_rc(launch_clear((cudaStream_t)stream, {ws, (size_t)kStatusBytes}));
-}
 
 }  // namespace
 
@@ -88,25 +87,23 @@ int gsa_cache_reserve(const gsa_cache_t* c, const int32_t* n_new, int32_t* start
 int gsa_cache_append(const gsa_cache_t* c, int32_t L_new, const void* K, const void* V, const void* g2_logits, const void* kI,
                      const int32_t* n_new, const int32_t* start, void* ws, size_t ws_bytes, void* stream) {
     CacheView v{};
-    int rc = check_cache(c, &v);
+    const int rc = check_cache(c, &v);
     if (rc) return rc;
     if (L_new < 1 || L_new > (int64_t)v.max_pages * v.T) return GSA_ERR_INVALID_ARG;
     if (!K || !V || !kI || !aligned32(K) || !aligned32(V) || !aligned16(kI)) return GSA_ERR_INVALID_ARG;
     if ((g2_logits && !aligned32(g2_logits)) || !n_new || !start || n_new == start) return GSA_ERR_INVALID_ARG;
     if (!ws_ok(ws, ws_bytes, list_ws_bytes(v))) return GSA_ERR_WORKSPACE;
-    if ((rc = clear_status(ws, stream))) return rc;
     return cuda_rc(launch_cache_append(v, L_new, (const bf16*)K, (const bf16*)V, (const bf16*)g2_logits, (const bf16*)kI, n_new, start,
                                        (int32_t*)ws, (cudaStream_t)stream));
 }
 
 int gsa_cache_read(const gsa_cache_t* c, int32_t L, void* K, void* V, void* kI, void* ws, size_t ws_bytes, void* stream) {
     CacheView v{};
-    int rc = check_cache(c, &v);
+    const int rc = check_cache(c, &v);
     if (rc) return rc;
     if (L < 1 || L > (int64_t)v.max_pages * v.T || (!K && !V && !kI)) return GSA_ERR_INVALID_ARG;
     if (!aligned32(K) || !aligned32(V) || !aligned16(kI)) return GSA_ERR_INVALID_ARG;
     if (!ws_ok(ws, ws_bytes, list_ws_bytes(v))) return GSA_ERR_WORKSPACE;
-    if ((rc = clear_status(ws, stream))) return rc;
     return cuda_rc(launch_cache_read(v, L, (bf16*)K, (bf16*)V, (bf16*)kI, (int32_t*)ws, (cudaStream_t)stream));
 }
 
@@ -121,11 +118,10 @@ int gsa_cache_fork(const gsa_cache_t* c, const int32_t* src_of, int32_t share, v
 
 int gsa_cache_release(const gsa_cache_t* c, const int32_t* drop, void* ws, size_t ws_bytes, void* stream) {
     CacheView v{};
-    int rc = check_cache(c, &v);
+    const int rc = check_cache(c, &v);
     if (rc) return rc;
     if (!drop) return GSA_ERR_INVALID_ARG;
     if (!ws_ok(ws, ws_bytes, list_ws_bytes(v))) return GSA_ERR_WORKSPACE;
-    if ((rc = clear_status(ws, stream))) return rc;
     return cuda_rc(launch_cache_release(v, drop, (int32_t*)ws, (cudaStream_t)stream));
 }
 
@@ -145,11 +141,8 @@ int gsa_cache_indexer_scores(const gsa_cache_t* c, const gsa_params_t* p, const 
     if (rc) return rc;
     if (!qI || !w || !scores || !aligned16(qI) || !aligned16(w) || !aligned16(scores)) return GSA_ERR_INVALID_ARG;
     if (row_stride < p->Lk || row_stride % 4 != 0) return GSA_ERR_INVALID_ARG;
-    const RowRange rr{0, p->B, 0, p->Lq};
-    if ((int64_t)p->B * p->Lq > 65535) return GSA_ERR_UNSUPPORTED_SHAPE;
     if (!ws_ok(ws, ws_bytes, list_ws_bytes(v))) return GSA_ERR_WORKSPACE;
-    if ((rc = clear_status(ws, stream))) return rc;
-    return cuda_rc(launch_cache_indexer(v, *p, rr, (const bf16*)qI, w, bI, scores, row_stride, (int32_t*)ws, (cudaStream_t)stream));
+    return cuda_rc(launch_cache_indexer(v, *p, (const bf16*)qI, w, bI, scores, row_stride, (int32_t*)ws, (cudaStream_t)stream));
 }
 
 int gsa_cache_topk(const gsa_cache_t* c, const gsa_params_t* p, const float* scores, int64_t row_stride, int32_t* idx, int32_t* kt,
@@ -160,7 +153,8 @@ int gsa_cache_topk(const gsa_cache_t* c, const gsa_params_t* p, const float* sco
     if (!scores || !idx || !kt || !aligned16(scores) || !aligned16(idx)) return GSA_ERR_INVALID_ARG;
     if (row_stride < p->Lk || row_stride % 4 != 0) return GSA_ERR_INVALID_ARG;
     if (!ws_ok(ws, ws_bytes, list_ws_bytes(v))) return GSA_ERR_WORKSPACE;
-    if ((rc = clear_status(ws, stream))) return rc;
+    // (the fallback counter in the head counts up)
+    if ((rc = cuda_rc(launch_clear((cudaStream_t)stream, {ws, (size_t)kStatusBytes})))) return rc;
     const RowRange rr{0, p->B, 0, p->Lq};
     const IdxLayout il{0, 0, p->Lq};
     return cuda_rc(launch_select(*p, rr, scores, row_stride, idx, kt, var, il, (int32_t*)ws + kStatusFallbackWord,

@@ -360,25 +360,29 @@ __global__ void __launch_bounds__(256) gsa_cache_compact_copy_kernel(const Cache
     copy_pages(c, ws + kStatusBytes / 4, moves);
 }
 
-__global__ void __launch_bounds__(256) gsa_cache_release_kernel(const CacheView c, const int32_t* __restrict__ drop, int32_t* dev_status) {
+__global__ void __launch_bounds__(256) gsa_cache_release_kernel(const CacheView c, const int32_t* __restrict__ drop, int32_t* __restrict__ ws) {
     chain_wait();
-    const int b = blockIdx.x;
-    if (!drop[b]) return;
-    const int n = min(max(c.lens[b], 0), c.max_pages << c.log_t);
-    for (int j = threadIdx.x; j < c.max_pages; j += 256) {
-        int32_t* at = c.table + (int64_t)b * c.max_pages + j;
-        if (j < pages_of(c, n)) {
-            const int page = *at;
-            if ((uint32_t)page >= (uint32_t)c.n_pages) report_bad_index(dev_status);
-            else if (atomicSub(c.refs + page, 1) <= 0) {       // (counts that do not match the tables)
-                atomicAdd(c.refs + page, 1);
-                report_bad_index(dev_status);
+    bool bad = false;
+    for (int b = blockIdx.x; b < c.B; b += gridDim.x) {
+        if (!drop[b]) continue;
+        const int len = c.lens[b], cap = c.max_pages << c.log_t, n = pages_of(c, min(max(len, 0), cap));
+        bad |= len < 0 || len > cap;
+        for (int j = threadIdx.x; j < c.max_pages; j += 256) {
+            int32_t* at = c.table + (int64_t)b * c.max_pages + j;
+            if (j < n) {
+                const int page = *at;
+                if ((uint32_t)page >= (uint32_t)c.n_pages) bad = true;
+                else if (atomicSub(c.refs + page, 1) <= 0) {       // (counts that do not match the tables)
+                    atomicAdd(c.refs + page, 1);
+                    bad = true;
+                }
             }
+            *at = -1;
         }
-        *at = -1;
+        __syncthreads();                         // (everybody has read the length)
+        if (threadIdx.x == 0) c.lens[b] = 0;
     }
-    __syncthreads();
-    if (threadIdx.x == 0) c.lens[b] = 0;
+    write_flags(ws, bad);
 }
 
 size_t plan_smem(const CacheView& c) { return sizeof(PlanShared) + (size_t)(c.n_pages + 31) / 32 * 4; }
@@ -410,8 +414,8 @@ cudaError_t launch_cache_fork(const CacheView& c, const int32_t* src_of, bool sh
     return cudaGetLastError();
 }
 
-cudaError_t launch_cache_release(const CacheView& c, const int32_t* drop, int32_t* dev_status, cudaStream_t st) {
-    launch_chained(gsa_cache_release_kernel, c.B, 256, 0, st, c, drop, dev_status);
+cudaError_t launch_cache_release(const CacheView& c, const int32_t* drop, int32_t* ws, cudaStream_t st) {
+    launch_chained(gsa_cache_release_kernel, c.B < kMaxFlags ? c.B : kMaxFlags, 256, 0, st, c, drop, ws);
     ++g_launches;
     return cudaGetLastError();
 }
