@@ -24,7 +24,8 @@
 //
 // Records come by asynchronous copies into a ring of kStages tiles a warp (2304 bytes each at d_h = 128), so that some 100 KB of an SM
 // are in flight.  Indices and pages are looked up for blocks of four or eight tiles, each warp of a unit a share of the keys, two blocks
-// ahead; the records' addresses pass through shared memory.
+// ahead; the records' addresses pass through shared memory.  The units of an SM are kept abreast, a barrier a block: left alone, the warps
+// that the scheduler prefers finish a quarter earlier than the others, which then have the SM half empty.
 //
 // Work split: the tiles of all rows, one after another, are dealt to the units in equal runs, whatever the sets' sizes (each CTA sums
 // up the budgets for itself).  A row that lies within one unit's run is finished there; the others' parts (at most two a unit) go to
@@ -38,16 +39,15 @@ namespace gsa {
 
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 16;                 // one CTA an SM
 constexpr int kTile = 16;                  // keys
 constexpr int kStages = 4;                 // tiles of a warp's ring: one being computed on, the others in flight
 constexpr int kMinTiles = 2;               // fewest tiles worth a unit of their own
 constexpr int kMaxSplitRows = 2048;        // rows of one launch, whose budgets a CTA sums up (16 KB of its shared memory)
 constexpr int kAddressBlocks = 3;          // blocks of record addresses: being read, next, being written
-constexpr int kCtasPerSm = 2;
 constexpr int kMergeWarps = 8;
 constexpr float kRefUnder = 7.0f;          // a new softmax reference lies 2^7 under the score that moved it there,
-constexpr float kRefSlack = 15.0f;         // and moves again when a score lies 2^15 above it (fp16 ends at 2^16)
+constexpr float kMostNumerator = 32768.0f; // and moves again when a score lies 2^15 above it (fp16 ends at 2^16)
 
 struct CacheAttnArgs {
     CacheView c;
@@ -59,7 +59,8 @@ struct CacheAttnArgs {
     int32_t units;                         // of the launch; as many as there are tiles for take part
     float* state;                          // [2 * units][n_h][d_h] numerators
     float2* stats;                         // [2 * units][n_h] reference, sum
-    int32_t* cum;                          // [rows + 1] tiles in front of each row, written for the merge
+    int4* merges;                          // [merge_items] rows whose parts the merge puts together: row, first slot, parts
+    int32_t merge_items, by_cut;           // one for each row, or (by_cut) for each border between units
     int32_t* flags;                        // [CTAs] whether one met something out of range
     int32_t* status;                       // head of the workspace
 };
@@ -191,8 +192,37 @@ constexpr size_t address_bytes(int NKV) { return (size_t)(kWarps / NKV) * kAddre
 template <int DH, int NKV>
 constexpr size_t fixed_smem() { return address_bytes(NKV) + (size_t)kWarps * kStages * Stage<DH>::kBytes; }
 
+// What the merge has to do: a row whose tiles lie in several units' runs has its first part in the unit that holds its first tile and the
+// others in the units behind it.  With by_cut an item is a border between units, and a row's item is the first border inside it.
+__device__ __forceinline__ void list_merges(const CacheAttnArgs& a, const int32_t* cum, int32_t tiles, int32_t units) {
+    for (int i = threadIdx.x; i < a.merge_items; i += kWarps * 32) {
+        int4 m = make_int4(0, 0, 0, 0);
+        int32_t row = i;
+        bool real = true;
+        if (a.by_cut) {
+            const int32_t u = i + 1;
+            real = u < units;
+            if (real) {
+                const int32_t x = first_tile(u, tiles, units);
+                int32_t rl = 0, rh = a.rows - 1;
+                while (rl < rh) {
+                    const int32_t mid = (rl + rh + 1) >> 1;
+                    if (cum[mid] <= x) rl = mid; else rh = mid - 1;
+                }
+                row = rl;
+                real = cum[row] != x && first_tile(u - 1, tiles, units) <= cum[row];
+            }
+        }
+        if (real && cum[row + 1] > cum[row]) {
+            const int32_t u0 = unit_of(cum[row], tiles, units);
+            m = make_int4(row, 2 * u0 + (cum[row] > first_tile(u0, tiles, units) ? 1 : 0), unit_of(cum[row + 1] - 1, tiles, units) - u0 + 1, 0);
+        }
+        a.merges[i] = m;                   // (one part, or none: nothing to do)
+    }
+}
+
 template <int DH, int G, int NKV>
-__global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) gsa_cache_attn_kernel(const CacheAttnArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const CacheAttnArgs a) {
     chain_wait();
     using St = Stage<DH>;
     constexpr int D = NKV * DH;
@@ -254,6 +284,8 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) gsa_cache_attn_kernel
         __syncthreads();
     }
     const int32_t units = units_for(tiles, gridDim.x * SUBS);
+    if (blockIdx.x == gridDim.x - 1) list_merges(a, cum, tiles, units);
+    const int32_t n_most = units ? (tiles + units - 1) / units : 0;        // of any unit
     int32_t lo = 0, n = 0;                 // this unit's tiles: lo .. lo + n - 1
     if (unit < units) {
         lo = first_tile(unit, tiles, units);
@@ -266,43 +298,57 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) gsa_cache_attn_kernel
             if (cum[m] <= lo) row = m; else rh = m - 1;
         }
 
+        // the first row's Q is on its way while the tables are read
+        constexpr bool kAll = !COLS || G == 4;
+        const bool q_mine = kAll || ((gid >> 1) == tig && (gid & 1) < G);          // COLS: this lane's index is this lane's column's slot
+        const int q_head = !COLS ? gid : G == 4 ? gid & 3 : gid & 1;
+        uint4 q[KW];
+        auto load_q = [&](int32_t of_row) {
+            const __nv_bfloat16* qp = a.Q + ((int64_t)of_row * a.n_h + h * G + (q_mine ? q_head : 0)) * DH + tig * (DH / 4);
+#pragma unroll
+            for (int w = 0; w < KW; ++w) q[w] = q_mine ? __ldg(reinterpret_cast<const uint4*>(qp) + w) : make_uint4(0u, 0u, 0u, 0u);
+        };
+        load_q(row);
+
         // ---- addresses of the records: a block's indices, then pages ----
         int32_t look_row = row;            // (of this lane's last key)
-        int32_t raw[STEPS], raw_row[STEPS], page[STEPS], pos[STEPS];
+        struct Look { int32_t raw, seq, len, pos, page; };     // a key: index, sequence and its length; position (-1: none) and page
         auto key_of = [&](int step) { return h * KPW + step * 32 + lane; };          // in the block
-        auto load_indices = [&](int block) {
+        auto load_indices = [&](Look(&k)[STEPS], int block) {
 #pragma unroll
             for (int st = 0; st < STEPS; ++st) {
-                raw_row[st] = -1;
+                k[st].seq = -1;
                 const int t = block * BT + key_of(st) / kTile;                         // tile of the run
                 if ((KPW < 32 && lane >= KPW) || t >= n) continue;
                 const int32_t g = lo + t;
                 while (cum[look_row + 1] <= g) ++look_row;
                 const int j = (g - cum[look_row]) * kTile + (lane & (kTile - 1));
                 // places behind the set's end read the tile's first key again (their probabilities are 0)
-                raw[st] = __ldg(a.idx + (int64_t)look_row * a.k_max + (j < budget[look_row] ? j : j & ~(kTile - 1)));
-                raw_row[st] = look_row;
+                k[st].raw = __ldg(a.idx + (int64_t)look_row * a.k_max + (j < budget[look_row] ? j : j & ~(kTile - 1)));
+                k[st].seq = (a.row0 + look_row) / a.Lq;
+                k[st].len = __ldg(c.lens + k[st].seq);
             }
         };
-        auto load_pages = [&]() {
+        auto load_pages = [&](Look(&k)[STEPS]) {
 #pragma unroll
             for (int st = 0; st < STEPS; ++st) {
-                page[st] = -1;
-                if (raw_row[st] < 0) continue;
-                const int32_t b = (a.row0 + raw_row[st]) / a.Lq, len = checked_len(c, b, a.Lk, bad);
-                pos[st] = raw[st];
-                if ((uint32_t)pos[st] >= (uint32_t)len) {
-                    bad = true;
-                    pos[st] = min(max(pos[st], 0), max(len - 1, 0));
-                }
-                page[st] = checked_page(c, b, pos[st], bad);
+                k[st].pos = -1;
+                if (k[st].seq < 0) continue;
+                const int32_t len = min(max(k[st].len, 0), a.Lk);
+                bad |= len != k[st].len || (uint32_t)k[st].raw >= (uint32_t)len;
+                k[st].pos = min(max(k[st].raw, 0), max(len - 1, 0));
+                k[st].page = __ldg(c.table + (int64_t)k[st].seq * c.max_pages + (k[st].pos >> c.log_t));
             }
         };
-        auto put_addresses = [&](int slot) {
+        auto put_addresses = [&](const Look(&k)[STEPS], int slot) {
 #pragma unroll
             for (int st = 0; st < STEPS; ++st)
-                if (page[st] >= 0)
-                    addresses[slot * (BT * kTile) + key_of(st)] = (int64_t)page[st] * c.page_bytes + (int64_t)(pos[st] & (c.T - 1)) * c.rec;
+                if (k[st].pos >= 0) {
+                    const bool named = (uint32_t)k[st].page < (uint32_t)c.n_pages;
+                    bad |= !named;
+                    addresses[slot * (BT * kTile) + key_of(st)] =
+                        (int64_t)(named ? k[st].page : 0) * c.page_bytes + (int64_t)(k[st].pos & (c.T - 1)) * c.rec;
+                }
         };
         auto unit_sync = [&]() {
             if constexpr (NKV == 1) __syncwarp();
@@ -327,13 +373,15 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) gsa_cache_attn_kernel
             cp_async_commit();             // (one group a tile, possibly empty)
         };
 
-        load_indices(0);
-        load_pages();
-        put_addresses(0);
-        if (n > BT) {
-            load_indices(1);
-            load_pages();
-            put_addresses(1);
+        Look look[STEPS];
+        {
+            Look second[STEPS];
+            load_indices(look, 0);
+            load_indices(second, 1);
+            load_pages(look);
+            load_pages(second);
+            put_addresses(look, 0);
+            put_addresses(second, 1);
         }
         unit_sync();
         int next = 0;                      // tile in the address ring (BT tiles a block) of the next one to copy
@@ -351,83 +399,76 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) gsa_cache_attn_kernel
         float q_scale = a.scale_log2;
         float o[MT][4], m_run[2], l_run[2];
         int32_t row_first = cum[row], row_end = cum[row + 1], row_k = budget[row];
-        bool fresh = true;
+        auto start_row = [&]() {           // Q into its operand registers, an empty state
+            if constexpr (!COLS) {
+#pragma unroll
+                for (int w = 0; w < KW; ++w) {
+                    qf[w][0] = __byte_perm(q[w].x, q[w].z, 0x5410); qf[w][1] = __byte_perm(q[w].x, q[w].z, 0x7632);
+                    qf[w][2] = __byte_perm(q[w].y, q[w].w, 0x5410); qf[w][3] = __byte_perm(q[w].y, q[w].w, 0x7632);
+                }
+            } else {
+                // the exponent of the warp's largest finite |q|
+                uint32_t top = 0;
+#pragma unroll
+                for (int w = 0; w < KW; ++w) {
+                    const uint32_t x[4] = {q[w].x, q[w].y, q[w].z, q[w].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t lo_e = (x[e] >> 7) & 255u, hi_e = (x[e] >> 23) & 255u;
+                        top = max(top, max(lo_e == 255u ? 0u : lo_e, hi_e == 255u ? 0u : hi_e));
+                    }
+                }
+                top = max(__reduce_max_sync(0xFFFFFFFFu, top), 20u);
+                const float up = __uint_as_float((127u + 14u + 127u - top) << 23);
+                q_scale = a.scale_log2 * 16777216.0f / up;                         // (2^24: what a code's place is worth)
+                float sum[KS];
+#pragma unroll
+                for (int gr = 0; gr < KS; ++gr) sum[gr] = 0.f;
+#pragma unroll
+                for (int w = 0; w < KW; ++w) {
+                    float f[8];
+                    const uint32_t x[4] = {q[w].x, q[w].y, q[w].z, q[w].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        f[2 * e] = __uint_as_float(x[e] << 16) * up;
+                        f[2 * e + 1] = __uint_as_float(x[e] & 0xFFFF0000u) * up;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[w / (KW / KS)] += f[e];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) qf[w][e] = (e & 1) ? pack_f16(f[e] * 0.0625f, f[e + 4] * 0.0625f) : pack_f16(f[e], f[e + 4]);
+                }
+                // this lane's columns: slot tig, heads 0 and 1; with four heads slot 2 set + (tig >> 1), heads 2 (tig & 1), + 1
+#pragma unroll
+                for (int set = 0; set < SETS; ++set)
+#pragma unroll
+                    for (int gr = 0; gr < KS; ++gr)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int from_slot = G == 4 ? 2 * set + (tig >> 1) : tig;
+                            const int from_gid = G == 4 ? 2 * (tig & 1) + e : 2 * tig + e;
+                            q_start[set][gr][e] = -8.0f / 16777216.0f * __shfl_sync(0xFFFFFFFFu, sum[gr], from_gid * 4 + from_slot);
+                        }
+            }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) o[mt][0] = o[mt][1] = o[mt][2] = o[mt][3] = 0.f;
+            m_run[0] = m_run[1] = -INFINITY;
+            l_run[0] = l_run[1] = 0.f;
+        };
         uint32_t st_off = 0;
         int slot = 1, in_block = 0, block = 0;                 // block's last written slot of addresses, tile in the block
+        start_row();
         for (int32_t i = 0; i < n; ++i) {
-            if (fresh) {
-                fresh = false;
-                const bool mine = COLS ? (G == 4 ? true : (gid >> 1) == tig && (gid & 1) < G) : true;
-                const int head = COLS ? (G == 4 ? gid & 3 : (gid & 1)) : gid;
-                const __nv_bfloat16* qp = a.Q + ((int64_t)row * a.n_h + h * G + (mine ? head : 0)) * DH + tig * (DH / 4);
-                uint4 q[KW];
-#pragma unroll
-                for (int w = 0; w < KW; ++w) q[w] = mine ? __ldg(reinterpret_cast<const uint4*>(qp) + w) : make_uint4(0u, 0u, 0u, 0u);
-                if constexpr (!COLS) {
-#pragma unroll
-                    for (int w = 0; w < KW; ++w) {
-                        qf[w][0] = __byte_perm(q[w].x, q[w].z, 0x5410); qf[w][1] = __byte_perm(q[w].x, q[w].z, 0x7632);
-                        qf[w][2] = __byte_perm(q[w].y, q[w].w, 0x5410); qf[w][3] = __byte_perm(q[w].y, q[w].w, 0x7632);
-                    }
-                } else {
-                    // the exponent of the warp's largest finite |q|
-                    uint32_t top = 0;
-#pragma unroll
-                    for (int w = 0; w < KW; ++w) {
-                        const uint32_t x[4] = {q[w].x, q[w].y, q[w].z, q[w].w};
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t lo_e = (x[e] >> 7) & 255u, hi_e = (x[e] >> 23) & 255u;
-                            top = max(top, max(lo_e == 255u ? 0u : lo_e, hi_e == 255u ? 0u : hi_e));
-                        }
-                    }
-                    top = max(__reduce_max_sync(0xFFFFFFFFu, top), 20u);
-                    const float up = __uint_as_float((127u + 14u + 127u - top) << 23);
-                    q_scale = a.scale_log2 * 16777216.0f / up;                         // (2^24: what a code's place is worth)
-                    float sum[KS];
-#pragma unroll
-                    for (int gr = 0; gr < KS; ++gr) sum[gr] = 0.f;
-#pragma unroll
-                    for (int w = 0; w < KW; ++w) {
-                        float f[8];
-                        const uint32_t x[4] = {q[w].x, q[w].y, q[w].z, q[w].w};
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            f[2 * e] = __uint_as_float(x[e] << 16) * up;
-                            f[2 * e + 1] = __uint_as_float(x[e] & 0xFFFF0000u) * up;
-                        }
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) sum[w / (KW / KS)] += f[e];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) qf[w][e] = (e & 1) ? pack_f16(f[e] * 0.0625f, f[e + 4] * 0.0625f) : pack_f16(f[e], f[e + 4]);
-                    }
-                    // this lane's columns: slot tig, heads 0 and 1; with four heads slot 2 set + (tig >> 1), heads 2 (tig & 1), + 1
-#pragma unroll
-                    for (int set = 0; set < SETS; ++set)
-#pragma unroll
-                        for (int gr = 0; gr < KS; ++gr)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int from_slot = G == 4 ? 2 * set + (tig >> 1) : tig;
-                                const int from_gid = G == 4 ? 2 * (tig & 1) + e : 2 * tig + e;
-                                q_start[set][gr][e] = -8.0f / 16777216.0f * __shfl_sync(0xFFFFFFFFu, sum[gr], from_gid * 4 + from_slot);
-                            }
-                }
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) o[mt][0] = o[mt][1] = o[mt][2] = o[mt][3] = 0.f;
-                m_run[0] = m_run[1] = -INFINITY;
-                l_run[0] = l_run[1] = 0.f;
-            }
             // ---- addresses ahead ----
             if (in_block == 0) {
-                if (block >= 1 && (block + 1) * BT < n) {
+                if (block >= 1 && (block + 1) * BT < n_most) {
                     slot = slot + 1 == kAddressBlocks ? 0 : slot + 1;
-                    put_addresses(slot);
-                    unit_sync();
+                    put_addresses(look, slot);
+                    __syncthreads();
                 }
-                if ((block + 2) * BT < n) load_indices(block + 2);
+                if ((block + 2) * BT < n) load_indices(look, block + 2);
             } else if (in_block == BT / 2) {
-                if ((block + 2) * BT < n) load_pages();
+                if ((block + 2) * BT < n) load_pages(look);
             }
             if (++in_block == BT) { in_block = 0; ++block; }
             cp_async_wait<kStages - 2>();  // this tile's records have landed
@@ -518,22 +559,28 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) gsa_cache_attn_kernel
 
             // ---- softmax against a reference that few scores move ----
             const int left = row_k - (lo + i - row_first) * kTile;             // keys of this tile, if below 16
-            float sc[4];
+            if (left < kTile) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                sc[e] = gid < left ? s[e] * q_scale : -INFINITY;
-                sc[2 + e] = gid + 8 < left ? s[2 + e] * q_scale : -INFINITY;
+                for (int e = 0; e < 2; ++e) {
+                    if (gid >= left) s[e] = -INFINITY;
+                    if (gid + 8 >= left) s[2 + e] = -INFINITY;
+                }
             }
-            const bool jump = fmaxf(sc[0], sc[2]) > m_run[0] + kRefSlack || fmaxf(sc[1], sc[3]) > m_run[1] + kRefSlack;
-            if (__any_sync(0xFFFFFFFFu, jump)) {
+            float p[4];
+            auto numerators = [&]() {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[e] = ex2(fmaf(s[e], q_scale, -m_run[e & 1]));
+            };
+            numerators();
+            if (__any_sync(0xFFFFFFFFu, fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])) > kMostNumerator)) {
                 float alpha[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float mx = fmaxf(sc[e], sc[2 + e]);
+                    float mx = fmaxf(s[e], s[2 + e]);
                     mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
                     mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
-                    const float m_new = fmaxf(m_run[e], mx - kRefUnder);
+                    const float m_new = fmaxf(m_run[e], fmaf(mx, q_scale, -kRefUnder));
                     alpha[e] = ex2(m_run[e] - m_new);
                     m_run[e] = m_new;
                     l_run[e] *= alpha[e];
@@ -542,14 +589,10 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) gsa_cache_attn_kernel
                 for (int mt = 0; mt < MT; ++mt) {
                     o[mt][0] *= alpha[0]; o[mt][1] *= alpha[1]; o[mt][2] *= alpha[0]; o[mt][3] *= alpha[1];
                 }
+                numerators();
             }
-            float p[4];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                p[e] = ex2(sc[e] - m_run[e]);
-                p[2 + e] = ex2(sc[2 + e] - m_run[e]);
-                l_run[e] += p[e] + p[2 + e];
-            }
+            l_run[0] += p[0] + p[2];
+            l_run[1] += p[1] + p[3];
             // (with groups in columns every lane of a key has its scores; the columns of P are those of the heads that there are)
             const bool head_cols = !COLS || 2 * tig < G;
             const uint32_t pb0 = transposed(head_cols ? pack_f16(p[0], p[1]) : 0u), pb1 = transposed(head_cols ? pack_f16(p[2], p[3]) : 0u);
@@ -579,6 +622,11 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) gsa_cache_attn_kernel
 
             // ---- end of the row, or of this unit's part of it ----
             if (lo + i + 1 == row_end || i + 1 == n) {
+                int32_t next_row = row;
+                if (i + 1 < n) {
+                    do ++next_row; while (cum[next_row + 1] <= row_end);           // (rows with an empty set are passed over)
+                    load_q(next_row);
+                }
                 float l[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
@@ -610,17 +658,15 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) gsa_cache_attn_kernel
                         }
                     }
                 }
-                fresh = true;
                 if (i + 1 < n) {
-                    do ++row; while (cum[row + 1] <= row_end);             // (rows with an empty set are passed over)
+                    row = next_row;
                     row_first = row_end; row_end = cum[row + 1]; row_k = budget[row];
+                    start_row();
                 }
             }
         }
     }
-    // what the merge needs, and rows with an empty set
-    if (blockIdx.x == 0)
-        for (int r = threadIdx.x; r <= a.rows; r += kWarps * 32) a.cum[r] = cum[r];
+    // rows with an empty set
     const int64_t row_vec = (int64_t)a.n_h * DH / 8;
     for (int r = blockIdx.x; r < a.rows; r += gridDim.x)
         if (budget[r] == 0)
@@ -631,10 +677,9 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) gsa_cache_attn_kernel
 }
 
 // Rows whose parts lie in several units' runs: the parts' states in their order, normalised, gated, rounded.  WPI warps share a
-// (row, head): all eight of a CTA where a row has many parts, one where it has few.  With by_cut the rows are found by the borders between
-// units instead of one by one, and a row is done at the first border inside it.  The last CTA writes the status head.
+// (row, head): all eight of a CTA where a row has many parts, one where it has few.  The last CTA writes the status head.
 template <int DH, int WPI>
-__global__ void __launch_bounds__(kMergeWarps * 32) gsa_cache_merge_kernel(const CacheAttnArgs a, int32_t by_cut, int32_t items, int32_t ctas) {
+__global__ void __launch_bounds__(kMergeWarps * 32) gsa_cache_merge_kernel(const CacheAttnArgs a, int32_t ctas) {
     chain_wait();
     constexpr int N = DH / 32;             // d of a lane
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -649,27 +694,15 @@ __global__ void __launch_bounds__(kMergeWarps * 32) gsa_cache_merge_kernel(const
     __shared__ float part_o[WPI > 1 ? WPI : 1][DH];
     __shared__ float2 part_ml[WPI > 1 ? WPI : 1];
     const int item = blockIdx.x * (kMergeWarps / WPI) + warp / WPI, sub = warp % WPI;
-    if (item >= items) return;             // (WPI > 1: one item a CTA, and there are no more CTAs than items)
+    if (item >= a.merge_items * a.n_h) return;             // (WPI > 1: one item a CTA, and there are no more CTAs than items)
     const int head = item % a.n_h;
-    int32_t row = item / a.n_h;
-    const int32_t tiles = a.cum[a.rows], units = units_for(tiles, a.units);
-    if (by_cut) {
-        const int32_t u = row + 1;
-        if (u >= units) return;
-        const int32_t x = first_tile(u, tiles, units);
-        int32_t rl = 0, rh = a.rows - 1;
-        while (rl < rh) {
-            const int32_t m = (rl + rh + 1) >> 1;
-            if (a.cum[m] <= x) rl = m; else rh = m - 1;
-        }
-        row = rl;
-        if (a.cum[row] == x || first_tile(u - 1, tiles, units) > a.cum[row]) return;
-    }
-    const int32_t c0 = a.cum[row], c1 = a.cum[row + 1];
-    if (c1 <= c0) return;                  // (an empty set: written by the first kernel)
-    const int32_t u0 = unit_of(c0, tiles, units), n = unit_of(c1 - 1, tiles, units) - u0 + 1;
-    if (n == 1) return;                    // (within one unit)
-    const int32_t first_slot = 2 * u0 + (c0 > first_tile(u0, tiles, units) ? 1 : 0);
+    const int4 todo = a.merges[item / a.n_h];
+    const int32_t row = todo.x, first_slot = todo.y, u0 = todo.y >> 1, n = todo.z;
+    if (n < 2) return;
+    const int64_t at_out = ((int64_t)row * a.n_h + head) * DH + lane * N;
+    uint32_t gate[N / 2];
+#pragma unroll
+    for (int d = 0; d < N / 2; ++d) gate[d] = __ldg(reinterpret_cast<const uint32_t*>(a.g1 + at_out) + d);
     float m = -INFINITY, l = 0.f, o[N];
 #pragma unroll
     for (int d = 0; d < N; ++d) o[d] = 0.f;
@@ -733,18 +766,14 @@ __global__ void __launch_bounds__(kMergeWarps * 32) gsa_cache_merge_kernel(const
                 for (int d = 0; d < N; ++d) o[d] = fmaf(part_o[w][lane * N + d], f, o[d]);
             }
     }
-    const int64_t at = ((int64_t)row * a.n_h + head) * DH + lane * N;
-    const uint32_t* g = reinterpret_cast<const uint32_t*>(a.g1 + at);
     const float inv = 1.0f / l;
 #pragma unroll
-    for (int d = 0; d < N; d += 2) {
-        const uint32_t gw = __ldg(g + d / 2);
-        reinterpret_cast<uint32_t*>(a.out + at)[d / 2] = pack_bf16(o[d] * inv * fast_sigmoid(__uint_as_float(gw << 16)),
-                                                                   o[d + 1] * inv * fast_sigmoid(__uint_as_float(gw & 0xFFFF0000u)));
-    }
+    for (int d = 0; d < N; d += 2)
+        reinterpret_cast<uint32_t*>(a.out + at_out)[d / 2] =
+            pack_bf16(o[d] * inv * fast_sigmoid(__uint_as_float(gate[d / 2] << 16)), o[d + 1] * inv * fast_sigmoid(__uint_as_float(gate[d / 2] & 0xFFFF0000u)));
 }
 
-int32_t unit_count(const gsa_params_t& p) { return sm_count() * kCtasPerSm * (kWarps / p.n_kv); }
+int32_t unit_count(const gsa_params_t& p) { return sm_count() * (kWarps / p.n_kv); }
 
 template <int DH, int G, int NKV>
 cudaError_t launch_main(const CacheAttnArgs& a, cudaStream_t st) {
@@ -778,22 +807,23 @@ cudaError_t launch_groups(const CacheAttnArgs& a, cudaStream_t st) {
 }
 
 template <int DH, int WPI>
-cudaError_t launch_merge(const CacheAttnArgs& a, int32_t by_cut, int32_t items, cudaStream_t st) {
-    const unsigned ctas = (unsigned)((items + kMergeWarps / WPI - 1) / (kMergeWarps / WPI)) + 1u;
-    cudaError_t e = launch_chained(gsa_cache_merge_kernel<DH, WPI>, ctas, kMergeWarps * 32, 0, st, a, by_cut, items, a.units / (kWarps / a.c.n_kv));
+cudaError_t launch_merge(const CacheAttnArgs& a, cudaStream_t st) {
+    const int32_t items = a.merge_items * a.n_h, per = kMergeWarps / WPI;
+    cudaError_t e = launch_chained(gsa_cache_merge_kernel<DH, WPI>, (unsigned)((items + per - 1) / per + 1), kMergeWarps * 32, 0, st, a,
+                                   a.units / (kWarps / a.c.n_kv));
     ++g_launches;
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-struct Plan { size_t stats, cum, flags, total; };
+struct Plan { size_t stats, merges, flags, total; };
 Plan plan_scratch(const gsa_params_t& p) {
     const size_t slots = 2 * (size_t)unit_count(p);
-    const int64_t all = (int64_t)p.B * p.Lq, rows = all < kMaxSplitRows ? all : kMaxSplitRows;
+    const int64_t rows = (int64_t)p.B * p.Lq, borders = unit_count(p);
     Plan w;
     w.stats = align_up(slots * p.n_h * p.d_h * 4, 256);
-    w.cum = w.stats + align_up(slots * p.n_h * 8, 256);
-    w.flags = w.cum + align_up((size_t)(rows + 1) * 4, 256);
-    w.total = w.flags + align_up((size_t)sm_count() * kCtasPerSm * 4, 256);
+    w.merges = w.stats + align_up(slots * p.n_h * 8, 256);
+    w.flags = w.merges + align_up((size_t)(rows < borders ? rows : borders) * 16, 256);
+    w.total = w.flags + align_up((size_t)sm_count() * 4, 256);
     return w;
 }
 
@@ -808,22 +838,22 @@ cudaError_t launch_cache_attn(const CacheView& c, const gsa_params_t& p, const _
     a.scale_log2 = (p.sm_scale > 0.f ? p.sm_scale : 1.0f / sqrtf((float)p.d_h)) * 1.4426950408889634f;
     const Plan w = plan_scratch(p);
     char* s = (char*)ws + kStatusBytes;
-    a.status = ws; a.state = (float*)s; a.stats = (float2*)(s + w.stats); a.cum = (int32_t*)(s + w.cum); a.flags = (int32_t*)(s + w.flags);
+    a.status = ws; a.state = (float*)s; a.stats = (float2*)(s + w.stats); a.merges = (int4*)(s + w.merges); a.flags = (int32_t*)(s + w.flags);
     const int32_t all = p.B * p.Lq, subs = kWarps / p.n_kv;
     for (int32_t r0 = 0; r0 < all; r0 += kMaxSplitRows) {
         const int64_t at = (int64_t)r0 * p.n_h * p.d_h;
         a.row0 = r0; a.rows = all - r0 < kMaxSplitRows ? all - r0 : kMaxSplitRows;
         a.Q = Q + at; a.g1 = g1 + at; a.out = out + at; a.idx = idx + (int64_t)r0 * p.k_max; a.kt = kt + r0;
-        // no more CTAs than the largest sets would keep busy
-        const int64_t most = units_for((int64_t)a.rows * ((p.k_max + kTile - 1) / kTile), unit_count(p));
-        a.units = (int32_t)((most + subs - 1) / subs * subs);
+        // no more CTAs than the largest sets would keep busy, one unit each to begin with
+        const int32_t most = units_for((int64_t)a.rows * ((p.k_max + kTile - 1) / kTile), unit_count(p));
+        a.units = (most < sm_count() ? most : sm_count()) * subs;
+        a.by_cut = a.rows > a.units - 1 ? 1 : 0;
+        a.merge_items = a.by_cut ? a.units - 1 : a.rows;
         cudaError_t e = p.d_h == 128 ? launch_groups<128>(a, st) : launch_groups<64>(a, st);
         if (e != cudaSuccess) return e;
-        const int32_t by_cut = a.rows > a.units - 1 ? 1 : 0;
-        const int32_t items = (by_cut ? a.units - 1 : a.rows) * p.n_h;
-        const bool many = !by_cut && a.units >= 8 * a.rows;        // parts of a row: eight or more
-        if (p.d_h == 128) e = many ? launch_merge<128, 8>(a, by_cut, items, st) : launch_merge<128, 1>(a, by_cut, items, st);
-        else e = many ? launch_merge<64, 8>(a, by_cut, items, st) : launch_merge<64, 1>(a, by_cut, items, st);
+        const bool many = !a.by_cut && a.units >= 8 * a.rows;      // parts of a row: eight or more
+        if (p.d_h == 128) e = many ? launch_merge<128, 8>(a, st) : launch_merge<128, 1>(a, st);
+        else e = many ? launch_merge<64, 8>(a, st) : launch_merge<64, 1>(a, st);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
