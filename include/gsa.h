@@ -373,7 +373,7 @@ int gsa_forward_host(const gsa_params_t *p, const void *Q, const void *K, const 
  * A stored value has at most seven significant bits: it is exact in bf16.
  *
  * Supported: n_kv in {1, 2, 4, 8}; d_h in {64, 128}; dI in {32, 64}; page_tokens in {16, 32, 64, 128}; B <= 4096;
- * n_pages <= 2^20; max_pages * page_tokens < 2^24.
+ * n_pages <= 2^20; max_pages * page_tokens < 2^24; a pool of at most 64 GiB.
  *
  * What the device finds wrong -- a length outside [0, max_pages * page_tokens], a table entry outside [0, n_pages) where a
  * token is read, an index set entry outside [0, lens[b]) -- is reported through the status word (GSA_ERR_INDEX_RANGE) and

@@ -25,6 +25,7 @@ int check_geometry(const gsa_cache_t* c, CacheView* v) {
     v->rec = (int32_t)align_up((size_t)D + D / 8, 16);
     v->keys_off = v->T * v->rec;
     v->page_bytes = (int64_t)v->T * (v->rec + 2 * c->dI);
+    if (v->page_bytes * c->n_pages > 1ll << 36) return GSA_ERR_UNSUPPORTED_SHAPE;          // (the attention counts 16 bytes in 32 bits)
     return GSA_OK;
 }
 

@@ -41,10 +41,11 @@ namespace {
 
 constexpr int kWarps = 16;                 // one CTA an SM
 constexpr int kTile = 16;                  // keys
-constexpr int kStages = 4;                 // tiles of a warp's ring: one being computed on, the others in flight
+constexpr int kStages = 4;                 // tiles of a warp's ring: two being computed on, the others in flight (a power of two)
+constexpr int kLut = 256;                  // scales by their byte, as fp32
 constexpr int kMinTiles = 2;               // fewest tiles worth a unit of their own
 constexpr int kMaxSplitRows = 2048;        // rows of one launch, whose budgets a CTA sums up (16 KB of its shared memory)
-constexpr int kAddressBlocks = 3;          // blocks of record addresses: being read, next, being written
+constexpr int kAddressBlocks = 4;          // blocks of record addresses: being read, next, being written (and a power of two)
 constexpr int kMergeWarps = 8;
 constexpr float kRefUnder = 7.0f;          // a new softmax reference lies 2^7 under the score that moved it there,
 constexpr float kMostNumerator = 32768.0f; // and moves again when a score lies 2^15 above it (fp16 ends at 2^16)
@@ -103,11 +104,14 @@ __device__ __forceinline__ void lds_words(uint32_t (&v)[W], uint32_t p) {
     else
         asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v[0]) : "r"(p));
 }
-template <int BYTES>
-__device__ __forceinline__ uint32_t lds_small(uint32_t p) {
+__device__ __forceinline__ uint32_t lds_byte(uint32_t p) {
     uint32_t v;
-    if constexpr (BYTES == 2) asm volatile("{ .reg .u16 t; ld.shared.u16 t, [%1]; cvt.u32.u16 %0, t; }" : "=r"(v) : "r"(p));
-    else asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(p));
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(p));
+    return v;
+}
+__device__ __forceinline__ uint32_t lds_word(uint32_t p) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(p));
     return v;
 }
 template <int BYTES>
@@ -188,9 +192,9 @@ struct Stage {
 __host__ __device__ constexpr size_t row_table_bytes(int rows) { return ((size_t)(2 * rows + 1) * 4 + 15) / 16 * 16; }
 // tiles of a block of addresses: one or two keys a lane of the unit's warps
 constexpr int block_tiles(int NKV) { return NKV >= 4 ? 8 : 4; }
-constexpr size_t address_bytes(int NKV) { return (size_t)(kWarps / NKV) * kAddressBlocks * block_tiles(NKV) * kTile * 8; }
+constexpr size_t address_bytes(int NKV) { return (size_t)(kWarps / NKV) * kAddressBlocks * block_tiles(NKV) * kTile * 4; }
 template <int DH, int NKV>
-constexpr size_t fixed_smem() { return address_bytes(NKV) + (size_t)kWarps * kStages * Stage<DH>::kBytes; }
+constexpr size_t fixed_smem() { return kLut * 4 + address_bytes(NKV) + (size_t)kWarps * kStages * Stage<DH>::kBytes; }
 
 // What the merge has to do: a row whose tiles lie in several units' runs has its first part in the unit that holds its first tile and the
 // others in the units behind it.  With by_cut an item is a border between units, and a row's item is the first border inside it.
@@ -236,7 +240,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
     constexpr int BT = block_tiles(NKV), KPW = BT * kTile / NKV, STEPS = (KPW + 31) / 32;      // keys of a block that a warp looks up
     constexpr bool COLS = G <= 4;          // groups in columns of their own
     constexpr int SETS = G == 4 ? 2 : 1;   // MMAs that the four slots take
-    extern __shared__ __align__(16) unsigned char smem[];  // record addresses, rings, cum[rows + 1], budget[rows]
+    extern __shared__ __align__(16) unsigned char smem[];  // scales, record addresses, rings, cum[rows + 1], budget[rows]
     __shared__ int32_t warp_sum[kWarps];
     __shared__ int32_t cta_bad;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -244,12 +248,15 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
     const CacheView& c = a.c;
     const int h = warp % NKV, sub = warp / NKV;
     const int unit = sub * gridDim.x + blockIdx.x;
-    int64_t* const addresses = reinterpret_cast<int64_t*>(smem) + sub * (kAddressBlocks * BT * kTile);
-    const uint32_t ring = smem_u32(smem) + (uint32_t)address_bytes(NKV) + warp * (kStages * St::kBytes);
+    const uint32_t lut = smem_u32(smem);
+    uint32_t* const addresses = reinterpret_cast<uint32_t*>(smem) + kLut + sub * (kAddressBlocks * BT * kTile);       // in units of 16 bytes
+    const uint32_t ring = lut + kLut * 4 + (uint32_t)address_bytes(NKV) + warp * (kStages * St::kBytes);
     int32_t* const cum = reinterpret_cast<int32_t*>(smem + fixed_smem<DH, NKV>());
     int32_t* const budget = cum + a.rows + 1;
     bool bad = false;
     if (threadIdx.x == 0) cta_bad = 0;
+    if (threadIdx.x < kLut) reinterpret_cast<float*>(smem)[threadIdx.x] = scale_f32(threadIdx.x);
+    auto scale_at = [&](uint32_t p) { return __uint_as_float(lds_word(lut + lds_byte(p) * 4)); };      // the scale whose byte is there
 
     // ---- tiles in front of every row ----
     int32_t tiles = 0;
@@ -347,7 +354,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
                     const bool named = (uint32_t)k[st].page < (uint32_t)c.n_pages;
                     bad |= !named;
                     addresses[slot * (BT * kTile) + key_of(st)] =
-                        (int64_t)(named ? k[st].page : 0) * c.page_bytes + (int64_t)(k[st].pos & (c.T - 1)) * c.rec;
+                        (uint32_t)(named ? k[st].page : 0) * (uint32_t)(c.page_bytes >> 4) + (uint32_t)(k[st].pos & (c.T - 1)) * (uint32_t)(c.rec >> 4);
                 }
         };
         auto unit_sync = [&]() {
@@ -360,15 +367,15 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
         const uint32_t to_k = ring + ckey * St::kRow + cpiece * 16, to_v = ring + St::kV + ckey * St::kVRow + cpiece * 16;
         const uint32_t to_s = ring + St::kS + (lane & 15) * St::kSRow;
         // tile t of the run, whose addresses start at `from`, into stage `off`
-        auto issue = [&](bool real, const int64_t* from, uint32_t off) {
+        auto issue = [&](bool real, const uint32_t* from, uint32_t off) {
             if (real) {
 #pragma unroll
                 for (int i = 0; i < kTile / KPI; ++i) {
-                    const unsigned char* src = from_codes + from[ckey + i * KPI];
+                    const unsigned char* src = from_codes + (uint64_t)from[ckey + i * KPI] * 16u;
                     cp_async16(to_k + off + i * KPI * St::kRow, src);
                     cp_async16(to_v + off + i * KPI * St::kVRow, src + D / 2);
                 }
-                if (lane < kTile) copy_async<St::kSRow>(to_s + off, from_scales + from[lane]);
+                if (lane < kTile) copy_async<St::kSRow>(to_s + off, from_scales + (uint64_t)from[lane] * 16u);
             }
             cp_async_commit();             // (one group a tile, possibly empty)
         };
@@ -384,17 +391,15 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
             put_addresses(second, 1);
         }
         unit_sync();
-        int next = 0;                      // tile in the address ring (BT tiles a block) of the next one to copy
-        uint32_t next_off = 0;             // its stage
-        auto issue_next = [&](bool real) {
-            issue(real, addresses + next * kTile, next_off);
-            next = next + 1 == kAddressBlocks * BT ? 0 : next + 1;
-            next_off = next_off == (kStages - 1) * St::kBytes ? 0u : next_off + St::kBytes;
+        auto issue_tile = [&](int32_t t) {
+            issue(t < n, addresses + (t & (kAddressBlocks * BT - 1)) * kTile, (uint32_t)(t & (kStages - 1)) * St::kBytes);
         };
 #pragma unroll
-        for (int t = 0; t + 1 < kStages; ++t) issue_next(t < n);
+        for (int t = 0; t + 1 < kStages; ++t) issue_tile(t);
 
         uint32_t qf[KW][4];                // Q as the B operand
+        constexpr bool QPAIR = G == 4 && DH == 64;             // four heads: zeroed for either set ahead of time, where registers allow
+        uint32_t qz[QPAIR ? KW : 1][4];
         float q_start[SETS][KS][2];        // COLS: what the accumulators start from, -8 times the group's sum of Q
         float q_scale = a.scale_log2;
         float o[MT][4], m_run[2], l_run[2];
@@ -438,6 +443,15 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
 #pragma unroll
                     for (int e = 0; e < 4; ++e) qf[w][e] = (e & 1) ? pack_f16(f[e] * 0.0625f, f[e + 4] * 0.0625f) : pack_f16(f[e], f[e + 4]);
                 }
+                if constexpr (QPAIR) {
+#pragma unroll
+                    for (int w = 0; w < KW; ++w)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            qz[w][e] = 2 + (gid >> 2) == tig ? qf[w][e] : 0u;
+                            qf[w][e] = (gid >> 2) == tig ? qf[w][e] : 0u;
+                        }
+                }
                 // this lane's columns: slot tig, heads 0 and 1; with four heads slot 2 set + (tig >> 1), heads 2 (tig & 1), + 1
 #pragma unroll
                 for (int set = 0; set < SETS; ++set)
@@ -455,111 +469,119 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
             m_run[0] = m_run[1] = -INFINITY;
             l_run[0] = l_run[1] = 0.f;
         };
-        uint32_t st_off = 0;
-        int slot = 1, in_block = 0, block = 0;                 // block's last written slot of addresses, tile in the block
-        start_row();
-        for (int32_t i = 0; i < n; ++i) {
-            // ---- addresses ahead ----
-            if (in_block == 0) {
-                if (block >= 1 && (block + 1) * BT < n_most) {
-                    slot = slot + 1 == kAddressBlocks ? 0 : slot + 1;
-                    put_addresses(look, slot);
-                    __syncthreads();
-                }
-                if ((block + 2) * BT < n) load_indices(look, block + 2);
-            } else if (in_block == BT / 2) {
-                if ((block + 2) * BT < n) load_pages(look);
-            }
-            if (++in_block == BT) { in_block = 0; ++block; }
-            cp_async_wait<kStages - 2>();  // this tile's records have landed
-            __syncwarp();                  // (everybody's, and the stage of the tile before has been read)
-            issue_next(i + kStages - 1 < n);
-            const uint32_t st = ring + st_off;
-            st_off = st_off == (kStages - 1) * St::kBytes ? 0u : st_off + St::kBytes;
-
-            // ---- S^T = K Q^T ----
-            float s[4];
-            {
-                uint32_t kc[2][KW];
+        // S^T = K Q^T of the tile in stage `st`, in two steps: the products, and what the scales and slots make of them
+        constexpr int ACCS = COLS ? SETS * KS : 2;
+        auto multiply = [&](uint32_t st, float(&acc)[ACCS][4]) {
+            uint32_t kc[2][KW];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) lds_words<KW>(kc[e], st + (gid + 8 * e) * St::kRow + tig * (KW * 4));
-                if constexpr (COLS) {
-                    float acc[SETS][KS][4];
+            for (int e = 0; e < 2; ++e) lds_words<KW>(kc[e], st + (gid + 8 * e) * St::kRow + tig * (KW * 4));
+            if constexpr (COLS) {
 #pragma unroll
-                    for (int set = 0; set < SETS; ++set)
+                for (int set = 0; set < SETS; ++set)
 #pragma unroll
-                        for (int gr = 0; gr < KS; ++gr)
+                    for (int gr = 0; gr < KS; ++gr)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[set][gr][e] = q_start[set][gr][e & 1];
+                        for (int e = 0; e < 4; ++e) acc[set * KS + gr][e] = q_start[set][gr][e & 1];
 #pragma unroll
-                    for (int w = 0; w < KW; ++w) {
-                        uint32_t x[2][4];
+                for (int w = 0; w < KW; ++w) {
+                    uint32_t x[2][4];
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const uint32_t v = kc[e][w], v8 = v >> 8;
-                            x[e][0] = v & 0x000F000Fu; x[e][1] = v & 0x00F000F0u;
-                            x[e][2] = v8 & 0x000F000Fu; x[e][3] = v8 & 0x00F000F0u;
-                        }
-#pragma unroll
-                        for (int set = 0; set < SETS; ++set) {
-                            const bool on = G != 4 || 2 * set + (gid >> 2) == tig;     // four heads: Q of a set's two slots
-                            float(&ac)[4] = acc[set][w / (KW / KS)];
-                            mma_f16_16816(ac, x[0][0], x[1][0], x[0][1], x[1][1], on ? qf[w][0] : 0u, on ? qf[w][1] : 0u);
-                            mma_f16_16816(ac, x[0][2], x[1][2], x[0][3], x[1][3], on ? qf[w][2] : 0u, on ? qf[w][3] : 0u);
-                        }
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t v = kc[e][w], v8 = v >> 8;
+                        x[e][0] = v & 0x000F000Fu; x[e][1] = v & 0x00F000F0u;
+                        x[e][2] = v8 & 0x000F000Fu; x[e][3] = v8 & 0x00F000F0u;
                     }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[e] = 0.f;
 #pragma unroll
                     for (int set = 0; set < SETS; ++set) {
-                        const int sl = G == 4 ? 2 * set + (tig >> 1) : tig;
+                        // four heads: Q of a set's two slots
+                        auto qv = [&](int e) -> uint32_t {
+                            if constexpr (QPAIR) return set ? qz[w][e] : qf[w][e];
+                            return G != 4 || 2 * set + (gid >> 2) == tig ? qf[w][e] : 0u;
+                        };
+                        float(&ac)[4] = acc[set * KS + w / (KW / KS)];
+                        mma_f16_16816(ac, x[0][0], x[1][0], x[0][1], x[1][1], qv(0), qv(1));
+                        mma_f16_16816(ac, x[0][2], x[1][2], x[0][3], x[1][3], qv(2), qv(3));
+                    }
+                }
+            } else {
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const uint32_t ks = lds_small<KS>(st + St::kS + (gid + 8 * e) * St::kSRow + sl * KS);
+                for (int e = 0; e < 4; ++e) acc[0][e] = acc[1][e] = 0.f;
 #pragma unroll
-                            for (int gr = 0; gr < KS; ++gr) {
-                                const float f = scale_f32((ks >> (8 * gr)) & 255u);
-                                s[2 * e] = fmaf(acc[set][gr][2 * e], f, s[2 * e]);
-                                s[2 * e + 1] = fmaf(acc[set][gr][2 * e + 1], f, s[2 * e + 1]);
-                            }
+                for (int gr = 0; gr < KS; ++gr) {
+                    const uint32_t sa = scale_bf16x2(lds_byte(st + St::kS + gid * St::kSRow + tig * KS + gr));
+                    const uint32_t sb = scale_bf16x2(lds_byte(st + St::kS + (gid + 8) * St::kSRow + tig * KS + gr));
+                    const uint32_t za = zero_bf16x2(sa), zb = zero_bf16x2(sb);
+#pragma unroll
+                    for (int w = gr * (KW / KS); w < (gr + 1) * (KW / KS); ++w) {
+                        uint32_t pa[4], pb[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            pa[j] = fma_bf16x2(code_pair(kc[0][w], j), sa, za);
+                            pb[j] = fma_bf16x2(code_pair(kc[1][w], j), sb, zb);
                         }
+                        mma_bf16_16816(acc[0], pa[0], pb[0], pa[1], pb[1], qf[w][0], qf[w][1]);
+                        mma_bf16_16816(acc[1], pa[2], pb[2], pa[3], pb[3], qf[w][2], qf[w][3]);
                     }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (G != 4) s[e] += __shfl_xor_sync(0xFFFFFFFFu, s[e], 1);
-                        s[e] += __shfl_xor_sync(0xFFFFFFFFu, s[e], 2);
-                    }
-                } else {
-                    float s2[4] = {0.f, 0.f, 0.f, 0.f};
-                    uint32_t ks[2];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[e] = 0.f;
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) ks[e] = lds_small<KS>(st + St::kS + (gid + 8 * e) * St::kSRow + tig * KS);
-#pragma unroll
-                    for (int gr = 0; gr < KS; ++gr) {
-                        const uint32_t sa = scale_bf16x2((ks[0] >> (8 * gr)) & 255u), sb = scale_bf16x2((ks[1] >> (8 * gr)) & 255u);
-                        const uint32_t za = zero_bf16x2(sa), zb = zero_bf16x2(sb);
-#pragma unroll
-                        for (int w = gr * (KW / KS); w < (gr + 1) * (KW / KS); ++w) {
-                            uint32_t pa[4], pb[4];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                pa[j] = fma_bf16x2(code_pair(kc[0][w], j), sa, za);
-                                pb[j] = fma_bf16x2(code_pair(kc[1][w], j), sb, zb);
-                            }
-                            mma_bf16_16816(s, pa[0], pb[0], pa[1], pb[1], qf[w][0], qf[w][1]);
-                            mma_bf16_16816(s2, pa[2], pb[2], pa[3], pb[3], qf[w][2], qf[w][3]);
-                        }
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[e] += s2[e];
                 }
             }
+        };
+        auto scale_up = [&](uint32_t st, const float(&acc)[ACCS][4], float(&s)[4]) {
+            if constexpr (COLS) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[e] = 0.f;
+#pragma unroll
+                for (int set = 0; set < SETS; ++set) {
+                    const int sl = G == 4 ? 2 * set + (tig >> 1) : tig;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                        for (int gr = 0; gr < KS; ++gr) {
+                            const float f = scale_at(st + St::kS + (gid + 8 * e) * St::kSRow + sl * KS + gr);
+                            s[2 * e] = fmaf(acc[set * KS + gr][2 * e], f, s[2 * e]);
+                            s[2 * e + 1] = fmaf(acc[set * KS + gr][2 * e + 1], f, s[2 * e + 1]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (G != 4) s[e] += __shfl_xor_sync(0xFFFFFFFFu, s[e], 1);
+                    s[e] += __shfl_xor_sync(0xFFFFFFFFu, s[e], 2);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[e] = acc[0][e] + acc[1][e];
+            }
+        };
+        auto stage_of = [&](int32_t t) { return ring + (uint32_t)(t & (kStages - 1)) * St::kBytes; };
+        start_row();
+        float acc[ACCS][4], s[4];
+        cp_async_wait<kStages - 2>();
+        __syncwarp();
+        multiply(ring, acc);
+        scale_up(ring, acc, s);
+        for (int32_t i = 0; i < n; ++i) {
+            // ---- addresses ahead ----
+            if ((i & (BT - 1)) == 0) {
+                if (i >= BT && i + BT < n_most) {
+                    put_addresses(look, ((uint32_t)i / BT + 1) & (kAddressBlocks - 1));
+                    __syncthreads();
+                }
+                if (i + 2 * BT < n) load_indices(look, (int)((uint32_t)i / BT) + 2);
+            } else if ((i & (BT - 1)) == BT / 2) {
+                if (i - BT / 2 + 2 * BT < n) load_pages(look);
+            }
+            cp_async_wait<kStages - 3>();  // the next tile's records have landed
+            __syncwarp();                  // (everybody's, and the stage of the tile before has been read)
+            issue_tile(i + kStages - 1);
+            // The next tile's scores are under way while this one's softmax is: four warps a scheduler do not hide one another's latencies.
+            // (Behind a row's last tile they are formed again with the next row's Q; behind the last tile of all they are nothing.)
+            const uint32_t st = stage_of(i), st_next = stage_of(i + 1);
+            multiply(st_next, acc);
 
             // ---- softmax against a reference that few scores move ----
-            const int left = row_k - (lo + i - row_first) * kTile;             // keys of this tile, if below 16
-            if (left < kTile) {
+            const bool row_ends = lo + i + 1 == row_end;
+            if (row_ends) {
+                const int left = row_k - (lo + i - row_first) * kTile;         // keys of this tile
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     if (gid >= left) s[e] = -INFINITY;
@@ -605,7 +627,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
                 for (int e = 0; e < 4; ++e) {
                     const int key = 2 * tig + (e & 1) + 8 * (e >> 1);
                     lds_words<VW>(vc[e], st + St::kV + key * St::kVRow + gid * (VW * 4));
-                    vs[e] = scale_f32(lds_small<1>(st + St::kS + key * St::kSRow + DH / 16 + (DH == 128 ? gid : gid >> 1)));
+                    vs[e] = scale_at(st + St::kS + key * St::kSRow + DH / 16 + (DH == 128 ? gid : gid >> 1));
                 }
                 const uint32_t sa = pack_f16(vs[0], vs[1]), sb = pack_f16(vs[2], vs[3]);
 #pragma unroll
@@ -620,8 +642,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
                     }
             }
 
+            scale_up(st_next, acc, s);
+
             // ---- end of the row, or of this unit's part of it ----
-            if (lo + i + 1 == row_end || i + 1 == n) {
+            if (row_ends || i + 1 == n) {
                 int32_t next_row = row;
                 if (i + 1 < n) {
                     do ++next_row; while (cum[next_row + 1] <= row_end);           // (rows with an empty set are passed over)
@@ -662,6 +686,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
                     row = next_row;
                     row_first = row_end; row_end = cum[row + 1]; row_k = budget[row];
                     start_row();
+                    multiply(st_next, acc);
+                    scale_up(st_next, acc, s);
                 }
             }
         }

@@ -32,7 +32,7 @@ def test_sizes(lib, n_kv, d_h, dI, T):
 @pytest.mark.parametrize("over,rc", [(dict(B=0), -1), (dict(n_pages=0), -1), (dict(max_pages=0), -1), (dict(B=4097), -2),
                                      (dict(n_pages=(1 << 20) + 1), -2), (dict(page_tokens=48), -2), (dict(page_tokens=256), -2),
                                      (dict(n_kv=3), -2), (dict(n_kv=16), -2), (dict(d_h=96), -2), (dict(dI=16), -2),
-                                     (dict(max_pages=1 << 20), -2)])
+                                     (dict(max_pages=1 << 20), -2), (dict(n_kv=8, d_h=128, dI=64, page_tokens=64, n_pages=1 << 20), -2)])
 def test_geometries_that_are_refused(lib, over, rc):
     c = gsa.cache_geometry(**{**GEO, **over})
     n = ctypes.c_size_t(0)
