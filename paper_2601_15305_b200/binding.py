@@ -327,30 +327,29 @@ def gsa_profile_set_events(ev_begin=None, ev_selected=None, ev_end=None) -> None
 
 
 # ---- the paged 4-bit cache ------------------------------------------------------------------------------------------
-# A decode step makes five of these calls: their arguments are checked with as little work on the host as that takes.
+# A decode step makes five of these calls: their arguments are checked with as little work on the host as that takes, and they go
+# through an extension of their own (csrc/gsa_call.c).
 class gsa_cache_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("pool", "table", "lens", "refs")] + \
                [(n, ctypes.c_int32) for n in ("n_pages", "page_tokens", "max_pages", "B", "n_kv", "d_h", "dI")]
 
 
-_PTR, _INT, _LONG, _SIZE = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
-# what stands between the cache and (workspace, its bytes, stream)
-_CACHE_ARGS = {
-    "gsa_cache_reserve": (_PTR, _PTR), "gsa_cache_append": (_INT,) + (_PTR,) * 6, "gsa_cache_read": (_INT, _PTR, _PTR, _PTR),
-    "gsa_cache_fork": (_PTR, _INT), "gsa_cache_release": (_PTR,), "gsa_cache_compact": (_PTR,),
-    "gsa_cache_indexer_scores": (_PTR,) * 5 + (_LONG,), "gsa_cache_topk": (_PTR, _PTR, _LONG, _PTR, _PTR, _PTR),
-    "gsa_cache_attn_fwd": (_PTR,) * 6,
-}
-_cache_fns = {}
+_call = None
+_addresses = {}
 
 
-def _cache_fn(name: str):
-    f = _cache_fns.get(name)
-    if f is None:
-        # (an object of its own: its argument types are nobody else's)
-        f = ctypes.CFUNCTYPE(_INT, _PTR, *_CACHE_ARGS[name], _PTR, _SIZE, _PTR)((name, lib()))
-        _cache_fns[name] = f
-    return f
+def _address(name: str) -> int:
+    """Where the library's function is; loads the extension that calls it (built with the library)."""
+    global _call
+    if _call is None:
+        lib()
+        try:
+            from ._gsa_call import call
+        except ImportError as e:
+            raise GsaError(f"{e}: build it with `python -m paper_2601_15305_b200.build`") from e
+        _call = call
+    a = _addresses[name] = ctypes.cast(getattr(lib(), name), ctypes.c_void_p).value
+    return a
 
 
 def cache_geometry(*, B: int, n_pages: int, page_tokens: int, max_pages: int, n_kv: int, d_h: int, dI: int) -> gsa_cache_t:
@@ -387,7 +386,8 @@ def _cache_call(name: str, c: gsa_cache_t, ws, stream, *args) -> None:
         raise GsaError("the cache, a contiguous workspace and the current device belong together")
     # (torch.cuda.current_stream() makes an object: 3 us, a fifth of a call)
     st = torch._C._cuda_getCurrentRawStream(c.device) if stream is None else stream.cuda_stream
-    rc = _cache_fn(name)(c.ref, *args, ws.data_ptr(), ws.nbytes, st)
+    at = _addresses.get(name) or _address(name)
+    rc = _call(at, c.ref, *args, ws.data_ptr(), ws.nbytes, st)
     if rc:
         _check(rc, name)
 
@@ -449,12 +449,12 @@ def gsa_cache_compact(c, live_pages, ws, stream=None) -> None:
 def gsa_cache_indexer_scores(c, p, qI, w, bI, scores, row_stride: int, ws, stream=None) -> None:
     d, B, Lq, HI = c.device, p.B, p.Lq, p.HI
     _cache_call("gsa_cache_indexer_scores", c, ws, stream, ctypes.addressof(p), _at(qI, BF16, (B, Lq, HI, p.dI), d),
-                _at(w, F32, (B, Lq, HI), d), _at(bI, F32, (HI,), d), _at(scores, F32, (B, Lq, row_stride), d), row_stride)
+                _at(w, F32, (B, Lq, HI), d), _at(bI, F32, (HI,), d), _at(scores, F32, (B, Lq, row_stride), d), int(row_stride))
 
 
 def gsa_cache_topk(c, p, scores, row_stride: int, idx, kt, var, ws, stream=None) -> None:
     d, rows = c.device, (p.B, p.Lq)
-    _cache_call("gsa_cache_topk", c, ws, stream, ctypes.addressof(p), _at(scores, F32, rows + (row_stride,), d), row_stride,
+    _cache_call("gsa_cache_topk", c, ws, stream, ctypes.addressof(p), _at(scores, F32, rows + (row_stride,), d), int(row_stride),
                 _at(idx, I32, rows + (p.k_max,), d), _at(kt, I32, rows, d), _at(var, F32, rows, d))
 
 

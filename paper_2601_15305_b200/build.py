@@ -1,16 +1,19 @@
-"""Builds libgsa_b200.so (the C-ABI library) in-tree with nvcc for sm_100a."""
+"""Builds libgsa_b200.so (the C-ABI library) in-tree with nvcc for sm_100a, and the small extension that calls it from Python."""
 from __future__ import annotations
 
 import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 CSRC = os.path.join(_PKG, "csrc")
 LIB_PATH = os.path.join(_PKG, "libgsa_b200.so")
+CALL_PATH = os.path.join(_PKG, "_gsa_call" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+CC = os.environ.get("CC", "gcc")
 
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
          "--expt-relaxed-constexpr", "-Xcompiler", "-fPIC", "-I", os.path.join(_ROOT, "include"), "-I", CSRC]
@@ -21,10 +24,10 @@ def sources():
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB_PATH):
+    if not os.path.exists(LIB_PATH) or not os.path.exists(CALL_PATH):
         return True
-    t = os.path.getmtime(LIB_PATH)
-    deps = sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(_ROOT, "include", "*.h"))
+    t = min(os.path.getmtime(LIB_PATH), os.path.getmtime(CALL_PATH))
+    deps = sources() + [os.path.join(CSRC, "gsa_call.c")] + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(_ROOT, "include", "*.h"))
     return any(os.path.getmtime(d) > t for d in deps)
 
 
@@ -49,6 +52,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
     tmp = LIB_PATH + f".tmp{os.getpid()}"
     subprocess.check_call([NVCC, "-shared", "-o", tmp, *objs, "-lcudart", "-ldl"])
     os.replace(tmp, LIB_PATH)
+    tmp = CALL_PATH + f".tmp{os.getpid()}"
+    subprocess.check_call([CC, "-O2", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "gsa_call.c"), "-o", tmp])
+    os.replace(tmp, CALL_PATH)
     return LIB_PATH
 
 

@@ -30,7 +30,8 @@
 // Work split: the tiles of all rows, one after another, are dealt to the units in equal runs, whatever the sets' sizes (each CTA sums
 // up the budgets for itself).  A row that lies within one unit's run is finished there; the others' parts (at most two a unit) go to
 // the workspace as softmax state and are merged by a second kernel, in order, so that nothing depends on scheduling.  More rows than
-// kMaxSplitRows take several such launches.
+// kMaxSplitRows take several such launches.  Small sets (kOwnTiles) in few rows have a CTA for each row instead, which merges its
+// units' parts itself: one launch.
 #include "gsa_cache.cuh"
 
 #include <cuda_fp16.h>
@@ -46,6 +47,7 @@ constexpr int kLut = 256;                  // scales by their byte, as fp32
 constexpr int kMinTiles = 2;               // fewest tiles worth a unit of their own
 constexpr int kMaxSplitRows = 2048;        // rows of one launch, whose budgets a CTA sums up (16 KB of its shared memory)
 constexpr int kAddressBlocks = 4;          // blocks of record addresses: being read, next, being written (and a power of two)
+constexpr int kOwnTiles = 2;               // tiles a unit, at most, for rows with a CTA of their own; twice as many if they occupy half the SMs
 constexpr int kMergeWarps = 8;
 constexpr float kRefUnder = 7.0f;          // a new softmax reference lies 2^7 under the score that moved it there,
 constexpr float kMostNumerator = 32768.0f; // and moves again when a score lies 2^15 above it (fp16 ends at 2^16)
@@ -64,6 +66,7 @@ struct CacheAttnArgs {
     int32_t merge_items, by_cut;           // one for each row, or (by_cut) for each border between units
     int32_t* flags;                        // [CTAs] whether one met something out of range
     int32_t* status;                       // head of the workspace
+    int32_t own;                           // a CTA for each row
 };
 
 // units that share `tiles` tiles; unit u has tiles first_tile(u) .. first_tile(u + 1) - 1
@@ -247,12 +250,16 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
     const int gid = lane >> 2, tig = lane & 3;
     const CacheView& c = a.c;
     const int h = warp % NKV, sub = warp / NKV;
-    const int unit = sub * gridDim.x + blockIdx.x;
+    const int rows = a.own ? 1 : a.rows, row_base = a.own ? blockIdx.x : 0;
+    const int unit = a.own ? sub : sub * gridDim.x + blockIdx.x;
     const uint32_t lut = smem_u32(smem);
     uint32_t* const addresses = reinterpret_cast<uint32_t*>(smem) + kLut + sub * (kAddressBlocks * BT * kTile);       // in units of 16 bytes
     const uint32_t ring = lut + kLut * 4 + (uint32_t)address_bytes(NKV) + warp * (kStages * St::kBytes);
+    // the part of a warp: numerators [G][d_h], reference and sum [G]
+    auto part_of = [&](int w) { return reinterpret_cast<float*>(smem + kLut * 4 + address_bytes(NKV) + (size_t)w * (kStages * St::kBytes)); };
+    float* const own_part = part_of(warp);
     int32_t* const cum = reinterpret_cast<int32_t*>(smem + fixed_smem<DH, NKV>());
-    int32_t* const budget = cum + a.rows + 1;
+    int32_t* const budget = cum + rows + 1;
     bool bad = false;
     if (threadIdx.x == 0) cta_bad = 0;
     if (threadIdx.x < kLut) reinterpret_cast<float*>(smem)[threadIdx.x] = scale_f32(threadIdx.x);
@@ -261,10 +268,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
     // ---- tiles in front of every row ----
     int32_t tiles = 0;
     {
-        const int per = (a.rows + kWarps * 32 - 1) / (kWarps * 32), r0 = min(a.rows, (int)threadIdx.x * per), r1 = min(a.rows, r0 + per);
+        const int per = (rows + kWarps * 32 - 1) / (kWarps * 32), r0 = min(rows, (int)threadIdx.x * per), r1 = min(rows, r0 + per);
         int32_t mine = 0;
         for (int r = r0; r < r1; ++r) {
-            const int32_t given = __ldg(a.kt + r), k = clamp_budget(given, a.k_max);
+            const int32_t given = __ldg(a.kt + row_base + r), k = clamp_budget(given, a.k_max);
             bad |= given != k;
             budget[r] = k;
             mine += (k + kTile - 1) / kTile;
@@ -287,11 +294,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
             cum[r] = at;
             at += (budget[r] + kTile - 1) / kTile;
         }
-        if (threadIdx.x == 0) cum[a.rows] = tiles;
+        if (threadIdx.x == 0) cum[rows] = tiles;
         __syncthreads();
     }
-    const int32_t units = units_for(tiles, gridDim.x * SUBS);
-    if (blockIdx.x == gridDim.x - 1) list_merges(a, cum, tiles, units);
+    const int32_t units = units_for(tiles, a.own ? SUBS : gridDim.x * SUBS);
+    if (!a.own && blockIdx.x == gridDim.x - 1) list_merges(a, cum, tiles, units);
     const int32_t n_most = units ? (tiles + units - 1) / units : 0;        // of any unit
     int32_t lo = 0, n = 0;                 // this unit's tiles: lo .. lo + n - 1
     if (unit < units) {
@@ -300,7 +307,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
     }
     if (n > 0) {
         int32_t row = 0;                   // the row that holds tile lo (of rows that start there the last: the others are empty)
-        for (int32_t rh = a.rows - 1; row < rh;) {
+        for (int32_t rh = rows - 1; row < rh;) {
             const int32_t m = (row + rh + 1) >> 1;
             if (cum[m] <= lo) row = m; else rh = m - 1;
         }
@@ -311,7 +318,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
         const int q_head = !COLS ? gid : G == 4 ? gid & 3 : gid & 1;
         uint4 q[KW];
         auto load_q = [&](int32_t of_row) {
-            const __nv_bfloat16* qp = a.Q + ((int64_t)of_row * a.n_h + h * G + (q_mine ? q_head : 0)) * DH + tig * (DH / 4);
+            const __nv_bfloat16* qp = a.Q + ((int64_t)(row_base + of_row) * a.n_h + h * G + (q_mine ? q_head : 0)) * DH + tig * (DH / 4);
 #pragma unroll
             for (int w = 0; w < KW; ++w) q[w] = q_mine ? __ldg(reinterpret_cast<const uint4*>(qp) + w) : make_uint4(0u, 0u, 0u, 0u);
         };
@@ -331,8 +338,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
                 while (cum[look_row + 1] <= g) ++look_row;
                 const int j = (g - cum[look_row]) * kTile + (lane & (kTile - 1));
                 // places behind the set's end read the tile's first key again (their probabilities are 0)
-                k[st].raw = __ldg(a.idx + (int64_t)look_row * a.k_max + (j < budget[look_row] ? j : j & ~(kTile - 1)));
-                k[st].seq = (a.row0 + look_row) / a.Lq;
+                k[st].raw = __ldg(a.idx + (int64_t)(row_base + look_row) * a.k_max + (j < budget[look_row] ? j : j & ~(kTile - 1)));
+                k[st].seq = (a.row0 + row_base + look_row) / a.Lq;
                 k[st].len = __ldg(c.lens + k[st].seq);
             }
         };
@@ -672,7 +679,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
                             const float inv = 1.0f / l[e];
 #pragma unroll
                             for (int d = 0; d < DL; ++d) v[d] *= inv;
-                            write_gated<DL>(a, ((int64_t)row * a.n_h + h * G + head) * DH + gid * DL, v);
+                            write_gated<DL>(a, ((int64_t)(row_base + row) * a.n_h + h * G + head) * DH + gid * DL, v);
+                        } else if (a.own) {
+                            // (into the warp's ring, which has done its work)
+                            float4* to = reinterpret_cast<float4*>(own_part + head * DH + gid * DL);
+#pragma unroll
+                            for (int d = 0; d < DL / 4; ++d) to[d] = make_float4(v[4 * d], v[4 * d + 1], v[4 * d + 2], v[4 * d + 3]);
+                            if (gid == 0) *reinterpret_cast<float2*>(own_part + G * DH + 2 * head) = make_float2(m_run[e], l[e]);
                         } else {
                             const int64_t sh = (int64_t)part * a.n_h + h * G + head;
                             float4* to = reinterpret_cast<float4*>(a.state + sh * DH + gid * DL);
@@ -692,11 +705,44 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
             }
         }
     }
+    if (a.own) {
+        __syncthreads();
+        if (units > 1) {
+            // the row's parts, in order: a warp a head, d_h / 32 of its values a lane
+            constexpr int N = DH / 32;
+            for (int head = warp; head < NKV * G; head += kWarps) {
+                float m = -INFINITY, l = 0.f, o[N];
+                for (int u = 0; u < units; ++u) m = fmaxf(m, part_of(u * NKV + head / G)[G * DH + 2 * (head % G)]);
+#pragma unroll
+                for (int d = 0; d < N; ++d) o[d] = 0.f;
+                for (int u = 0; u < units; ++u) {
+                    const float* part = part_of(u * NKV + head / G);
+                    const float w = ex2(part[G * DH + 2 * (head % G)] - m);
+                    l = fmaf(part[G * DH + 2 * (head % G) + 1], w, l);
+#pragma unroll
+                    for (int d = 0; d < N; ++d) o[d] = fmaf(part[(head % G) * DH + lane * N + d], w, o[d]);
+                }
+                const int64_t at = ((int64_t)row_base * a.n_h + head) * DH + lane * N;
+                const float inv = 1.0f / l;
+#pragma unroll
+                for (int d = 0; d < N; d += 2) {
+                    const uint32_t g = __ldg(reinterpret_cast<const uint32_t*>(a.g1 + at) + d / 2);
+                    reinterpret_cast<uint32_t*>(a.out + at)[d / 2] = pack_bf16(o[d] * inv * fast_sigmoid(__uint_as_float(g << 16)),
+                                                                               o[d + 1] * inv * fast_sigmoid(__uint_as_float(g & 0xFFFF0000u)));
+                }
+            }
+        }
+    }
     // rows with an empty set
     const int64_t row_vec = (int64_t)a.n_h * DH / 8;
-    for (int r = blockIdx.x; r < a.rows; r += gridDim.x)
+    for (int r = a.own ? 0 : blockIdx.x; r < rows; r += gridDim.x)
         if (budget[r] == 0)
-            for (int i = threadIdx.x; i < row_vec; i += kWarps * 32) reinterpret_cast<uint4*>(a.out)[r * row_vec + i] = make_uint4(0u, 0u, 0u, 0u);
+            for (int i = threadIdx.x; i < row_vec; i += kWarps * 32)
+                reinterpret_cast<uint4*>(a.out)[(row_base + r) * row_vec + i] = make_uint4(0u, 0u, 0u, 0u);
+    if (a.own) {
+        write_flags(a.status, bad);
+        return;
+    }
     if (bad) cta_bad = 1;
     __syncthreads();
     if (threadIdx.x == 0) a.flags[blockIdx.x] = cta_bad;
@@ -807,7 +853,7 @@ cudaError_t launch_main(const CacheAttnArgs& a, cudaStream_t st) {
     constexpr size_t fixed = fixed_smem<DH, NKV>();
     cudaError_t e = grant_smem(granted, reinterpret_cast<const void*>(gsa_cache_attn_kernel<DH, G, NKV>), fixed + row_table_bytes(kMaxSplitRows));
     if (e != cudaSuccess) return e;
-    e = launch_chained(gsa_cache_attn_kernel<DH, G, NKV>, (unsigned)(a.units / (kWarps / NKV)), kWarps * 32, fixed + row_table_bytes(a.rows), st, a);
+    e = launch_chained(gsa_cache_attn_kernel<DH, G, NKV>, (unsigned)(a.own ? a.rows : a.units / (kWarps / NKV)), kWarps * 32, fixed + row_table_bytes(a.own ? 1 : a.rows), st, a);
     ++g_launches;
     return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -866,6 +912,14 @@ cudaError_t launch_cache_attn(const CacheView& c, const gsa_params_t& p, const _
     char* s = (char*)ws + kStatusBytes;
     a.status = ws; a.state = (float*)s; a.stats = (float2*)(s + w.stats); a.merges = (int4*)(s + w.merges); a.flags = (int32_t*)(s + w.flags);
     const int32_t all = p.B * p.Lq, subs = kWarps / p.n_kv;
+    // A CTA for each row, or equal runs and a merge?  Measured (us, sets of k keys; own CTA / runs):  8 KV heads of 128, up to 32 rows: k 32
+    // 7.8 / 8.8, 64 9.5 / 9.1, 128 12.8 / 9.2;  128 rows: 64 9.9 / 11.9, 256 18.5 / 21.4;  one of 64, up to 32 rows: 256 7.0 / 7.5, 512 8.4 /
+    // 7.6;  two of 128, 128 rows: 256 11.1 / 16.9.  The launch that runs take more costs the host 2.4 us; rows of unequal sets favour runs.
+    if (all <= sm_count() && (p.k_max + kTile - 1) / kTile <= (2 * all >= sm_count() ? 2 : 1) * kOwnTiles * subs) {
+        a.own = 1; a.rows = all;
+        a.Q = Q; a.g1 = g1; a.out = out; a.idx = idx; a.kt = kt;
+        return p.d_h == 128 ? launch_groups<128>(a, st) : launch_groups<64>(a, st);
+    }
     for (int32_t r0 = 0; r0 < all; r0 += kMaxSplitRows) {
         const int64_t at = (int64_t)r0 * p.n_h * p.d_h;
         a.row0 = r0; a.rows = all - r0 < kMaxSplitRows ? all - r0 : kMaxSplitRows;

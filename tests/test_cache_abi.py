@@ -106,6 +106,21 @@ def test_arguments_that_are_refused(lib):
     assert lib.gsa_status_string(-8).decode().startswith("the cache")
 
 
+def test_calls_through_the_extension(lib):
+    """The same function by ctypes and by the extension; what it does not take."""
+    address = gsa._address("gsa_cache_page_bytes")
+    c, n, m = gsa.cache_geometry(**GEO), ctypes.c_size_t(0), ctypes.c_size_t(0)
+    assert lib.gsa_cache_page_bytes(ctypes.byref(c), ctypes.byref(n)) == 0
+    assert gsa._call(address, ctypes.addressof(c), ctypes.addressof(m)) == 0 and m.value == n.value > 0
+    assert gsa._call(address, ctypes.addressof(c), None) == -1 and gsa._call(address, None, None) == -1
+    # negative integers, and every argument in its place: reserve .. attn take up to ten
+    big, st = 1 << 40, 0
+    assert gsa._call(gsa._address("gsa_cache_append"), ctypes.addressof(c), -1, 0, 0, 0, 0, 0, 0, 0, big, st) == -1
+    for bad in ((), (0,), (address, 1.5), (address, "x"), (address,) + (0,) * 17):
+        with pytest.raises((TypeError, ValueError)):
+            gsa._call(*bad)
+
+
 def test_binding_checks_shapes_and_places():
     t = lambda *s, dtype=torch.int32: torch.zeros(*s, dtype=dtype)  # noqa: E731
     with pytest.raises(gsa.GsaError):
