@@ -8,7 +8,7 @@
 //     I[t, key]      = sum_head w[head] * sigmoid(S^T[key, head] + b[head])     (sum across the 4 lanes
 //                                                                               that hold a key's heads)
 // The kernel is bound by reading k^I once per query row: d^I * 2 bytes per (row, key).
-#include "gsa_indexer_rows.cuh"
+#include "gsa_common.cuh"
 
 namespace gsa {
 
@@ -30,6 +30,12 @@ struct RowsIdxArgs {
     int32_t act;
 };
 
+__device__ __forceinline__ void ldg32(const void* p, uint4& lo, uint4& hi) {
+    asm volatile("ld.global.nc.L1::no_allocate.v8.u32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(lo.x), "=r"(lo.y), "=r"(lo.z), "=r"(lo.w), "=r"(hi.x), "=r"(hi.y), "=r"(hi.z), "=r"(hi.w)
+                 : "l"(p));
+}
+
 template <int DI, int HI>
 __global__ void __launch_bounds__(kRowsWarps * 32) gsa_indexer_rows_kernel(const RowsIdxArgs a) {
     chain_wait();
@@ -43,27 +49,75 @@ __global__ void __launch_bounds__(kRowsWarps * 32) gsa_indexer_rows_kernel(const
     const int key_hi = min(n, key_lo + a.keys_per_cta);
     if (key_lo >= key_hi) return;
 
-    using Tile = KeyTile<DI>;
-    RowQuery<DI, HI> q;
-    q.load(a.qI, a.w, a.bI, (size_t)b * a.Lq + t, a.act, gid, tig);
+    // Lane tig owns the tig-th quarter of every key row (DI/4 consecutive elements); the B operand
+    // q^I[head = gid] is read with the same split, so both sides agree on which d a k-index means.
+    constexpr int LANE_ELEMS = DI / 4;                 // bf16 per lane and key: 16 (DI 64) or 8 (DI 32)
+    uint32_t qb[LANE_ELEMS / 2];
+    {
+        const __nv_bfloat16* qp = a.qI + (((size_t)b * a.Lq + t) * HI + (gid < HI ? gid : 0)) * DI + tig * LANE_ELEMS;
+#pragma unroll
+        for (int i = 0; i < LANE_ELEMS / 2; ++i)
+            qb[i] = gid < HI ? *reinterpret_cast<const uint32_t*>(qp + 2 * i) : 0u;
+    }
+    // heads 2*tig, 2*tig+1 are this lane's columns of S^T
+    float wv[2], bv[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int h = 2 * tig + e;
+        wv[e] = h < HI ? a.w[((size_t)b * a.Lq + t) * HI + h] : 0.f;
+        bv[e] = (a.bI && h < HI) ? a.bI[h] * (a.act == 1 ? 1.0f : -1.4426950408889634f) : 0.f;
+    }
     const unsigned char* kbase = reinterpret_cast<const unsigned char*>(a.kI) + (size_t)b * a.Lk * DI * 2 +
-                                 tig * (Tile::kElems * 2);
+                                 tig * (LANE_ELEMS * 2);
     float* __restrict__ out_row = a.scores + (int64_t)lr * a.row_stride;
 
     for (int k0 = key_lo + warp * 16 * kTilesPerStep; k0 < key_hi; k0 += kRowsWarps * 16 * kTilesPerStep) {
-        Tile ka[kTilesPerStep];
+        uint32_t ka[kTilesPerStep][2][LANE_ELEMS / 2];          // [tile][key gid / gid+8][packed pairs]
 #pragma unroll
         for (int u = 0; u < kTilesPerStep; ++u)
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
                 // rows past the end of the cache are clamped to the last one; their scores are not stored
                 const int key = min(k0 + u * 16 + hf * 8 + gid, a.Lk - 1);
-                ka[u].load(hf, kbase + (size_t)key * (DI * 2));
+                const unsigned char* kp = kbase + (size_t)key * (DI * 2);
+                if constexpr (LANE_ELEMS == 16) {
+                    uint4 lo, hi;
+                    ldg32(kp, lo, hi);
+                    ka[u][hf][0] = lo.x; ka[u][hf][1] = lo.y; ka[u][hf][2] = lo.z; ka[u][hf][3] = lo.w;
+                    ka[u][hf][4] = hi.x; ka[u][hf][5] = hi.y; ka[u][hf][6] = hi.z; ka[u][hf][7] = hi.w;
+                } else {
+                    const uint4 v = __ldg(reinterpret_cast<const uint4*>(kp));
+                    ka[u][hf][0] = v.x; ka[u][hf][1] = v.y; ka[u][hf][2] = v.z; ka[u][hf][3] = v.w;
+                }
             }
 #pragma unroll
         for (int u = 0; u < kTilesPerStep; ++u) {
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < LANE_ELEMS / 4; ++ks)          // one k-step uses 4 of the lane's elements
+                mma_bf16_16816(s, ka[u][0][2 * ks], ka[u][1][2 * ks], ka[u][0][2 * ks + 1], ka[u][1][2 * ks + 1],
+                               qb[2 * ks], qb[2 * ks + 1]);
+            // s[0], s[1]: key gid, heads 2tig, 2tig+1;  s[2], s[3]: key gid + 8
             float acc[2];
-            q.score(ka[u], a.act, acc);
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                float v = 0.f;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    if (a.act == 1) {                                     // Eq. 3: ReLU
+                        v = fmaf(wv[e], fmaxf(s[hf * 2 + e] + bv[e], 0.f), v);
+                    } else {
+                        float ex, rc;
+                        const float arg = fminf(fmaf(s[hf * 2 + e], -1.4426950408889634f, bv[e]), 80.f);
+                        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(ex) : "f"(arg));
+                        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rc) : "f"(1.0f + ex));
+                        v = fmaf(wv[e], rc, v);
+                    }
+                }
+                v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
+                v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);
+                acc[hf] = v;
+            }
             const int key = k0 + u * 16 + (tig & 1) * 8 + gid;
             if (tig < 2 && key < key_hi) out_row[key] = acc[tig & 1];
         }

@@ -56,14 +56,17 @@ struct SelectArgs {
     int32_t Lq, Lk;
     int32_t k_base, k_min, k_max, k_mode;
     float v_bar;
-    const int32_t* lens;      // keys of each sequence instead of Lk (nullable); a launch then does the rows that see
+    const int32_t* lens;      // LENS: keys of each sequence instead of Lk; a launch then does the rows that see
     int32_t n_lo, n_hi;       // n_lo < n <= n_hi keys, and those that see none if n_lo is 0
 };
 
-// visible keys of a row; false if the row belongs to another launch or, seeing nothing, has just been written
+// visible keys of a row; false if the row belongs to another launch or, seeing nothing, has just been written (LENS)
+template <bool LENS>
 __device__ __forceinline__ bool row_keys(const SelectArgs& a, int b, int t, int32_t* out_idx, int64_t orow, bool writer, int& n) {
-    n = a.Lk - a.Lq + t + 1;
-    if (!a.lens) return true;
+    if constexpr (!LENS) {
+        n = a.Lk - a.Lq + t + 1;
+        return true;
+    }
     n = min(max(__ldg(a.lens + b), 0), a.Lk) - a.Lq + t + 1;
     if (n <= 0 && a.n_lo == 0 && writer) {
         for (int i = threadIdx.x; i < a.k_max; i += blockDim.x) out_idx[i] = -1;
@@ -231,6 +234,7 @@ __device__ __forceinline__ int budget_from_var(const SelectArgs& a, double var, 
     return (int)fl;
 }
 
+template <bool LENS>
 __global__ void __launch_bounds__(kSelThreads, 2) gsa_select_kernel(const SelectArgs a, int q_first, int q_rows) {
     chain_wait();
     extern __shared__ __align__(16) unsigned char dyn_smem[];
@@ -244,7 +248,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) gsa_select_kernel(const Select
     const int64_t orow = a.il.row(b, t);
     int32_t* __restrict__ out_idx = a.idx + orow * a.k_max;
     int n;                                                   // visible keys
-    if (!row_keys(a, b, t, out_idx, orow, true, n)) return;
+    if (!row_keys<LENS>(a, b, t, out_idx, orow, true, n)) return;
     const int nchunks = (n + kIter - 1) / kIter;              // chunks of 512 consecutive scores (long rows)
     const bool listed = nchunks <= kMaxChunks;  // longer rows go straight to the whole-row path
     // the table of list segments has one entry per 128 scores (8 lanes of an iteration) while that fits,
@@ -623,7 +627,7 @@ struct ShortShared {
     int32_t k;
 };
 
-template <int NT, int CS>
+template <int NT, int CS, bool LENS>
 __global__ void __launch_bounds__(NT, 1024 / NT) gsa_select_short_kernel(const SelectArgs a, int q_first, int q_rows) {
     chain_wait();
     namespace cg = cooperative_groups;
@@ -641,14 +645,15 @@ __global__ void __launch_bounds__(NT, 1024 / NT) gsa_select_short_kernel(const S
         if constexpr (CS > 1) cg::this_cluster().sync();
         else __syncthreads();
     };
+    if constexpr (CS > 1 && !LENS) cg::this_cluster().barrier_arrive();        // (awaited before the first access to another CTA's memory)
     const int bl = item / q_rows;
     const int t = q_first + q_rows - 1 - item % q_rows;       // long rows first
     const int lr = bl * a.rr.R + (t - a.rr.q_begin);
     const int64_t orow = a.il.row(a.rr.b0 + bl, t);
     int32_t* __restrict__ out_idx = a.idx + orow * a.k_max;
     int n_row;                                                // visible keys, at most 32 NT CS
-    if (!row_keys(a, a.rr.b0 + bl, t, out_idx, orow, rank == 0, n_row)) return;       // (the same for all CTAs of a cluster)
-    if constexpr (CS > 1) cg::this_cluster().barrier_arrive();        // (awaited before the first access to another CTA's memory)
+    if (!row_keys<LENS>(a, a.rr.b0 + bl, t, out_idx, orow, rank == 0, n_row)) return;       // (the same for all CTAs of a cluster)
+    if constexpr (CS > 1 && LENS) cg::this_cluster().barrier_arrive();                       // (the same)
     const int slice = CS > 1 ? ((n_row + CS - 1) / CS + 127) / 128 * 128 : n_row;
     const int p0 = rank * slice;                              // this CTA's first position, and how many it has
     const int n = CS > 1 ? max(0, min(slice, n_row - p0)) : n_row;
@@ -921,12 +926,12 @@ __global__ void __launch_bounds__(256) gsa_all_visible_kernel(RowRange rr, IdxLa
     }
 }
 
-template <int NT, int CS>
+template <int NT, int CS, bool LENS = false>
 cudaError_t launch_short(const SelectArgs& a, int q_first, int q_rows, cudaStream_t st) {
     constexpr int smem = (int)sizeof(ShortShared<NT>);
-    cudaError_t e = cudaFuncSetAttribute(gsa_select_short_kernel<NT, CS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    cudaError_t e = cudaFuncSetAttribute(gsa_select_short_kernel<NT, CS, LENS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    launch_chained_cluster(CS, gsa_select_short_kernel<NT, CS>, (unsigned)(a.rr.nb * q_rows * CS), NT, smem, st, a, q_first, q_rows);
+    launch_chained_cluster(CS, gsa_select_short_kernel<NT, CS, LENS>, (unsigned)(a.rr.nb * q_rows * CS), NT, smem, st, a, q_first, q_rows);
     ++g_launches;
     return cudaGetLastError();
 }
@@ -958,18 +963,18 @@ cudaError_t launch_select(const gsa_params_t& p, RowRange rr, const float* score
     const int off = p.Lk - p.Lq;
     if (lens) {                                               // (known on the device only: the longest that a row may be decides)
         const int q0 = rr.q_begin, n_max = off + q0 + rr.R;
-        if (n_max <= 4096) return launch_short<128, 1>(a, q0, rr.R, st);
-        if (n_max <= 8192) return launch_short<256, 1>(a, q0, rr.R, st);
-        if (n_max <= 16384) return launch_short<512, 1>(a, q0, rr.R, st);
+        if (n_max <= 4096) return launch_short<128, 1, true>(a, q0, rr.R, st);
+        if (n_max <= 8192) return launch_short<256, 1, true>(a, q0, rr.R, st);
+        if (n_max <= 16384) return launch_short<512, 1, true>(a, q0, rr.R, st);
         if (n_max <= 32 * 512 * kRowCluster && (int64_t)rr.rows() * kRowCluster <= 2 * sm_count())
-            return launch_short<512, kRowCluster>(a, q0, rr.R, st);
+            return launch_short<512, kRowCluster, true>(a, q0, rr.R, st);
         a.n_hi = 16384;
-        cudaError_t e = launch_short<512, 1>(a, q0, rr.R, st);
+        cudaError_t e = launch_short<512, 1, true>(a, q0, rr.R, st);
         if (e != cudaSuccess) return e;
         a.n_lo = 16384; a.n_hi = INT32_MAX;
-        e = cudaFuncSetAttribute(gsa_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        e = cudaFuncSetAttribute(gsa_select_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
-        launch_chained(gsa_select_kernel, rr.rows(), kSelThreads, smem, st, a, q0, rr.R);
+        launch_chained(gsa_select_kernel<true>, rr.rows(), kSelThreads, smem, st, a, q0, rr.R);
         ++g_launches;
         return cudaGetLastError();
     }
@@ -987,9 +992,9 @@ cudaError_t launch_select(const gsa_params_t& p, RowRange rr, const float* score
     if (off + t_end <= 32 * 512 * kRowCluster && (int64_t)rr.nb * (t_end - t16) * kRowCluster <= 2 * sm_count())
         return launch_short<512, kRowCluster>(a, t16, t_end - t16, st);
     // (set on every call: the attribute belongs to the current device)
-    e = cudaFuncSetAttribute(gsa_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    e = cudaFuncSetAttribute(gsa_select_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    launch_chained(gsa_select_kernel, rr.nb * (t_end - t16), kSelThreads, smem, st, a, t16, t_end - t16);
+    launch_chained(gsa_select_kernel<false>, rr.nb * (t_end - t16), kSelThreads, smem, st, a, t16, t_end - t16);
     ++g_launches;
     return cudaGetLastError();
 }
