@@ -376,8 +376,11 @@ int gsa_forward_host(const gsa_params_t *p, const void *Q, const void *K, const 
  * n_pages <= 2^20; max_pages * page_tokens < 2^24; a pool of at most 64 GiB.
  *
  * What the device finds wrong -- a length outside [0, max_pages * page_tokens], a table entry outside [0, n_pages) where a
- * token is read, an index set entry outside [0, lens[b]) -- is reported through the status word (GSA_ERR_INDEX_RANGE) and
- * never becomes an address: reads are clamped into the pool (the results of that row are then meaningless), writes are skipped.
+ * token is read, an index set entry outside [0, lens[b]) -- is reported (GSA_ERR_INDEX_RANGE) and never becomes an address:
+ * reads are clamped into the pool (the results of that row are then meaningless), writes are skipped.  gsa_device_status on the
+ * call's workspace says so; these calls keep what they report in words behind the head as well, one for each CTA, which that
+ * call adds up: the head's first word alone does not tell.  A workspace may be used by one call after another in stream order,
+ * captured ones included; two calls that may run at the same time need one each.
  */
 typedef struct gsa_cache {
     void *pool;           /* n_pages * gsa_cache_page_bytes, 32-byte aligned                 */
@@ -450,11 +453,14 @@ int gsa_cache_compact(const gsa_cache_t *c, int32_t *live_pages, void *ws, size_
  * and q_begin / q_end are ignored.
  *
  * gsa_cache_indexer_scores: gsa_indexer_scores with k^I from the cache.  For few rows a sequence (decode): every row reads the
- *   sequence's k^I by itself; B * Lq <= 65535.  scores [B, Lq, row_stride], written for the visible keys.
+ *   sequence's k^I by itself.  scores [B, Lq, row_stride], written for the visible keys.
  * gsa_cache_topk: gsa_adaptive_topk for those rows.  A row that sees no key gets kt = 0 and var = 0.
  * gsa_cache_attn_fwd: gsa_sparse_gated_attn_fwd with K and V' from the cache.  Q, g1_logits, out [B, Lq, n_h, d_h] bf16,
  *   idx [B, Lq, k_max], kt [B, Lq]; the entries of a set may stand in any order.  A row with kt = 0 is written as zeros.
- *   Sums and softmax statistics are fp32; the probabilities are rounded to bf16 for their product with V'.
+ *   Sums and softmax statistics are fp32.  For the product with V' the softmax numerators are rounded to fp16, scaled so that a row's
+ *   largest lies between 2^7 and 2^15: to 2^-11 of one, or 2^-32 of the row's sum where that is more.  With up to four query heads a KV
+ *   head a finite |q| sm_scale of 2^117 and more may count as infinite.  An infinity or NaN in Q, or in a selected K, makes the head's
+ *   row NaN, one in a selected V' the 16 values that share its scale.
  *   ws: gsa_cache_attn_workspace_bytes(p).  The result does not depend on scheduling.
  */
 int gsa_cache_indexer_scores(const gsa_cache_t *c, const gsa_params_t *p, const void *qI, const float *w, const float *bI,
@@ -466,7 +472,7 @@ int gsa_cache_attn_fwd(const gsa_cache_t *c, const gsa_params_t *p, const void *
                        const int32_t *kt, void *out, void *ws, size_t ws_bytes, void *stream);
 
 /*
- * Waits for `stream`, reads the device status word at the start of `ws` into
+ * Waits for `stream`, reads the device status word at the start of `ws` (a gsa_cache_* call's, and the words behind it) into
  * *status_out (host) and returns GSA_OK, GSA_ERR_DEVICE_TIMEOUT (*status_out 1..3: copy producer,
  * MMA issuer, epilogue), GSA_ERR_INDEX_RANGE (*status_out 6) or GSA_ERR_CACHE_FULL (*status_out 7) accordingly.
  * The word is cleared by every call that takes `ws`.  ws == NULL reads the status word of

@@ -368,7 +368,7 @@ def make_cache(pool, table, lens, refs, *, page_tokens: int, n_kv: int, d_h: int
     if len({t.device for t in (pool, table, lens, refs)}) != 1:
         raise GsaError("a cache lives on one device")
     c.pool, c.table, c.lens, c.refs = _dp(pool, torch.uint8), _dp(table, I32), _dp(lens, I32), _dp(refs, I32)
-    c.tensors, c.device, c.ref = (pool, table, lens, refs), pool.get_device(), ctypes.addressof(c)
+    c.tensors, c.device = (pool, table, lens, refs), pool.get_device()
     return c
 
 
@@ -387,7 +387,7 @@ def _cache_call(name: str, c: gsa_cache_t, ws, stream, *args) -> None:
     # (torch.cuda.current_stream() makes an object: 3 us, a fifth of a call)
     st = torch._C._cuda_getCurrentRawStream(c.device) if stream is None else stream.cuda_stream
     at = _addresses.get(name) or _address(name)
-    rc = _call(at, c.ref, *args, ws.data_ptr(), ws.nbytes, st)
+    rc = _call(at, ctypes.addressof(c), *args, ws.data_ptr(), ws.nbytes, st)
     if rc:
         _check(rc, name)
 
@@ -417,7 +417,9 @@ def gsa_cache_reserve(c, n_new, start, ws, stream=None) -> None:
 
 def gsa_cache_append(c, K, V, g2, kI, n_new, start, ws, stream=None) -> None:
     """Row i < n_new[b] of K, V * sigmoid(g2) and kI to position start[b] + i of sequence b (g2 None: V already gated)."""
-    d, B, L = c.device, c.B, K.shape[1]
+    if kI is None or kI.dim() != 3:
+        raise GsaError("kI is [B, L_new, dI]")
+    d, B, L = c.device, c.B, kI.shape[1]
     kv = (B, L, c.n_kv, c.d_h)
     _cache_call("gsa_cache_append", c, ws, stream, L, _at(K, BF16, kv, d), _at(V, BF16, kv, d), _at(g2, BF16, kv, d),
                 _at(kI, BF16, (B, L, c.dI), d), _at(n_new, I32, (B,), d), _at(start, I32, (B,), d))
@@ -425,7 +427,10 @@ def gsa_cache_append(c, K, V, g2, kI, n_new, start, ws, stream=None) -> None:
 
 def gsa_cache_read(c, K, V, kI, ws, stream=None) -> None:
     """The cache as contiguous tensors [B, L, ...]; any of the three may be None; positions behind a sequence's end stay as they were."""
-    L = next(t for t in (K, V, kI) if t is not None).shape[1]
+    some = next((t for t in (K, V, kI) if t is not None), None)
+    if some is None or some.dim() < 2:
+        raise GsaError("K and V are [B, L, n_kv, d_h], kI [B, L, dI]; at least one of them is wanted")
+    L = some.shape[1]
     kv = (c.B, L, c.n_kv, c.d_h)
     _cache_call("gsa_cache_read", c, ws, stream, L, _at(K, BF16, kv, c.device), _at(V, BF16, kv, c.device),
                 _at(kI, BF16, (c.B, L, c.dI), c.device))

@@ -155,6 +155,7 @@ int gsa_cache_topk(const gsa_cache_t* c, const gsa_params_t* p, const float* sco
     if (row_stride < p->Lk || row_stride % 4 != 0) return GSA_ERR_INVALID_ARG;
     if (!ws_ok(ws, ws_bytes, list_ws_bytes(v))) return GSA_ERR_WORKSPACE;
     // (the fallback counter in the head counts up)
+    t_dev_status = (int32_t*)ws;
     if ((rc = cuda_rc(launch_clear((cudaStream_t)stream, {ws, (size_t)kStatusBytes})))) return rc;
     const RowRange rr{0, p->B, 0, p->Lq};
     const IdxLayout il{0, 0, p->Lq};

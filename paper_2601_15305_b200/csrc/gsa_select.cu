@@ -58,6 +58,7 @@ struct SelectArgs {
     float v_bar;
     const int32_t* lens;      // LENS: keys of each sequence instead of Lk; a launch then does the rows that see
     int32_t n_lo, n_hi;       // n_lo < n <= n_hi keys, and those that see none if n_lo is 0
+    int32_t* status;          // LENS: told of a length outside [0, Lk]
 };
 
 // visible keys of a row; false if the row belongs to another launch or, seeing nothing, has just been written (LENS)
@@ -67,7 +68,9 @@ __device__ __forceinline__ bool row_keys(const SelectArgs& a, int b, int t, int3
         n = a.Lk - a.Lq + t + 1;
         return true;
     }
-    n = min(max(__ldg(a.lens + b), 0), a.Lk) - a.Lq + t + 1;
+    const int32_t given = __ldg(a.lens + b), len = min(max(given, 0), a.Lk);
+    if (given != len && writer && threadIdx.x == 0) report_bad_index(a.status);
+    n = len - a.Lq + t + 1;
     if (n <= 0 && a.n_lo == 0 && writer) {
         for (int i = threadIdx.x; i < a.k_max; i += blockDim.x) out_idx[i] = -1;
         if (threadIdx.x == 0) {
@@ -956,7 +959,7 @@ cudaError_t launch_select(const gsa_params_t& p, RowRange rr, const float* score
     a.rr = rr; a.il = il; a.Lq = p.Lq; a.Lk = p.Lk;
     a.k_base = p.k_base; a.k_min = p.k_min; a.k_max = p.k_max; a.k_mode = p.k_mode; a.v_bar = p.v_bar;
 
-    a.lens = lens; a.n_lo = 0; a.n_hi = INT32_MAX;
+    a.lens = lens; a.n_lo = 0; a.n_hi = INT32_MAX; a.status = t_dev_status;
     const size_t smem = ((sizeof(SelShared) + 15) / 16) * 16;
 
     // rows by the number of scores they see: up to 4096, 8192, 16384, longer

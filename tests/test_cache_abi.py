@@ -132,6 +132,18 @@ def test_binding_checks_shapes_and_places():
         gsa.make_cache(t(n, dtype=torch.uint8), t(2, 5), t(2), t(10), page_tokens=16, n_kv=2, d_h=64, dI=32)
 
 
+def test_binding_refuses_calls_without_tensors():
+    c = gsa.cache_geometry(**GEO)
+    c.device = 0
+    x = torch.zeros(2, 3, 2, 64, dtype=torch.bfloat16)
+    n = torch.zeros(2, dtype=torch.int32)
+    ws = torch.zeros(1024, dtype=torch.uint8)
+    for call in (lambda: gsa.gsa_cache_append(c, x, x, None, None, n, n, ws), lambda: gsa.gsa_cache_append(c, x, x, None, x, n, n, ws),
+                 lambda: gsa.gsa_cache_read(c, None, None, None, ws), lambda: gsa.gsa_cache_read(c, n, None, None, ws)):
+        with pytest.raises(gsa.GsaError):
+            call()
+
+
 # ---- the plain form itself ---------------------------------------------------------------------------------------------------
 def test_plain_rounding_to_bf16():
     g = torch.Generator().manual_seed(1)

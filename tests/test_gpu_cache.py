@@ -598,6 +598,207 @@ def test_corrupt_sets_and_tables_are_reported_not_followed(damage):
         assert p.status() == 6
 
 
+@pytest.mark.parametrize("G", [1, 2, 4, 8])
+@pytest.mark.parametrize("geo", GEOMETRIES, ids=lambda g: "-".join(map(str, g.values())))
+def test_attention_of_large_sets_of_every_head_layout(geo, G):
+    """Sets too large for a CTA of their own: runs of tiles over all SMs, rows cut anywhere, empty rows between them."""
+    lens = [1300, 0, 5, 900, 0, 0, 401, 1300]
+    p = _filled(geo, lens, 40 + G)
+    sets = _random_sets(np.random.default_rng(G), lens, 2, [1200, 700, 1, 1, 3, 16, 899, 17, 1, 1, 0, 9, 400, 33, 1111, 1200], sort=G > 2)
+    Q, g1, out, status, _ = _attend(p, G, 2, sets, 1200)
+    assert status == 0
+    _check_rows(p, Q, g1, out, sets, 2, geo["d_h"] ** -0.5)
+    assert all((out[b, t] == 0).all() for b in range(8) for t in range(2) if len(sets[b][t]) == 0)
+
+
+@pytest.mark.parametrize("rows", [30, 73, 74, 148, 149])
+@pytest.mark.parametrize("k_max", [64, 65, 128, 129])
+def test_attention_on_both_sides_of_the_row_split(rows, k_max):
+    """Eight KV heads: two units a CTA, so that sets of 64 keys (128, where rows fill half the SMs) end the form with a CTA for each row."""
+    geo = GEOMETRIES[5]
+    p = _filled(geo, [rows + 150], 41)
+    sets = _random_sets(np.random.default_rng(k_max), [rows + 150], rows, [k_max, k_max, 1, 0, k_max - 15, 33])
+    Q, g1, out, status, _ = _attend(p, 2, rows, sets, k_max)
+    assert status == 0
+    _check_rows(p, Q, g1, out, sets, rows, 64 ** -0.5, rows={(0, t) for t in list(range(0, rows, 11)) + [rows - 2, rows - 1]})
+    assert not out.isnan().any()
+
+
+@pytest.mark.parametrize("G", [1, 4, 8])
+@pytest.mark.parametrize("k_max", [24, 600])
+def test_queries_that_are_not_finite_stay_in_their_head(G, k_max):
+    geo = GEOMETRIES[3]
+    p = _filled(geo, [700, 650], 42)
+    sets = _random_sets(np.random.default_rng(G), [700, 650], 1, [k_max, k_max - 3])
+    n_h = 4 * G
+    Q = torch.randn(2, 1, n_h, 128, generator=p.gen).to(BF16)
+    spoilt = Q.clone()
+    spoilt[0, 0, 1, 5], spoilt[0, 0, n_h - 1, 127], spoilt[1, 0, 0, 64] = float("inf"), float("nan"), -float("inf")
+    g1 = torch.randn(2, 1, n_h, 128, generator=p.gen).to(BF16)
+    idx, kt = np.full((2, 1, k_max), -1, np.int32), np.zeros((2, 1), np.int32)
+    for b in range(2):
+        kt[b, 0] = len(sets[b][0])
+        idx[b, 0, :kt[b, 0]] = sets[b][0]
+    gp = gsa.make_params(B=2, Lq=1, Lk=700, n_h=n_h, n_kv=4, d_h=128, HI=1, dI=32, k_base=1, k_min=1, k_max=k_max)
+    ws = torch.empty(gsa.gsa_cache_attn_workspace_bytes(gp), dtype=torch.uint8, device="cuda")
+    out = torch.zeros(2, 1, n_h, 128, dtype=BF16, device="cuda")
+    gsa.gsa_cache_attn_fwd(p.c, gp, spoilt.cuda(), g1.cuda(), i32(idx), i32(kt), out, ws)
+    assert gsa.gsa_device_status(ws) == 0
+    for b, h in ((0, 1), (0, n_h - 1), (1, 0)):
+        assert out[b, 0, h].isnan().all()
+        out[b, 0, h], Q[b, 0, h] = 0.0, 0.0
+        g1[b, 0, h] = -float("inf")                                      # (its row of the plain form: zeros)
+    _check_rows(p, Q, g1, out, sets, 1, 128 ** -0.5)
+
+
+@pytest.mark.parametrize("exponent", [-100, -20, 20, 40])
+def test_queries_of_any_magnitude(exponent):
+    """Scores are formed from Q times a power of two: very small and very large ones, heads of one group far apart, as exactly as others."""
+    geo = GEOMETRIES[4]
+    p = _filled(geo, [300], 43)
+    Q = torch.randn(1, 1, 4, 128, generator=p.gen) * 2.0 ** exponent
+    Q[0, 0, 1] *= 2.0 ** -10
+    g1 = torch.randn(1, 1, 4, 128, generator=p.gen).to(BF16)
+    gp = gsa.make_params(B=1, Lq=1, Lk=300, n_h=4, n_kv=1, d_h=128, HI=1, dI=64, k_base=1, k_min=1, k_max=300, sm_scale=2.0 ** -(exponent + 4))
+    out, ws = torch.zeros(1, 1, 4, 128, dtype=BF16, device="cuda"), torch.empty(gsa.gsa_cache_attn_workspace_bytes(gp), dtype=torch.uint8, device="cuda")
+    Q, s = Q.to(BF16), np.arange(0, 300, 2)
+    idx = np.full((1, 1, 300), -1, np.int32)
+    idx[0, 0, :150] = s
+    gsa.gsa_cache_attn_fwd(p.c, gp, Q.cuda(), g1.cuda(), i32(idx), i32([[150]]), out, ws)
+    assert gsa.gsa_device_status(ws) == 0
+    _check_rows(p, Q, g1, out, [[s]], 1, 2.0 ** -(exponent + 4))
+
+
+def test_a_sequence_longer_than_the_bound_is_reported_and_cut():
+    geo = GEOMETRIES[1]
+    p = _filled(geo, [100, 60], 44)
+    gp = gsa.make_params(B=2, Lq=1, Lk=64, n_h=1, n_kv=1, d_h=64, HI=1, dI=32, k_base=8, k_min=8, k_max=8, k_mode=2)
+    qI, w = torch.randn(2, 1, 1, 32, generator=p.gen).to(BF16).cuda(), torch.ones(2, 1, 1, device="cuda")
+    sc = torch.full((2, 1, 68), float("nan"), device="cuda")
+    gsa.gsa_cache_indexer_scores(p.c, gp, qI, w, None, sc, 68, p.ws)
+    assert p.status() == 6
+    assert sc[0, 0, :64].isfinite().all() and sc[0, 0, 64:].isnan().all() and sc[1, 0, :60].isfinite().all() and sc[1, 0, 60:].isnan().all()
+    idx, kt = torch.full((2, 1, 8), -7, dtype=I32, device="cuda"), torch.zeros(2, 1, dtype=I32, device="cuda")
+    gsa.gsa_cache_topk(p.c, gp, sc, 68, idx, kt, None, p.ws)
+    assert p.status() == 6 and (kt == 8).all() and int(idx.max()) < 64 and int(idx.min()) >= 0
+    for b, n in ((0, 64), (1, 60)):
+        assert idx[b, 0].tolist() == torch.sort(torch.sort(sc[b, 0, :n], descending=True, stable=True).indices[:8]).values.tolist()
+    Q = torch.randn(2, 1, 1, 64, generator=p.gen).to(BF16).cuda()
+    out, ws = torch.zeros_like(Q), torch.empty(gsa.gsa_cache_attn_workspace_bytes(gp), dtype=torch.uint8, device="cuda")
+    gsa.gsa_cache_attn_fwd(p.c, gp, Q, Q, idx, kt, out, ws)
+    assert gsa.gsa_device_status(ws) == 6 and out.isfinite().all()
+    # and a negative length: nothing visible, reported by all three
+    p.lens[0] = -3
+    gsa.gsa_cache_topk(p.c, gp, sc, 68, idx, kt, None, p.ws)
+    assert p.status() == 6 and kt.flatten().tolist() == [0, 8] and (idx[0] == -1).all()
+    gsa.gsa_cache_indexer_scores(p.c, gp, qI, w, None, sc, 68, p.ws)
+    assert p.status() == 6
+    # the next call that finds nothing wrong says so
+    p.lens[0] = 64
+    gsa.gsa_cache_topk(p.c, gp, sc, 68, idx, kt, None, p.ws)
+    assert p.status() == 0
+    gsa.gsa_cache_attn_fwd(p.c, gp, Q, Q, idx, kt, out, ws)
+    assert gsa.gsa_device_status(ws) == 0
+
+
+@pytest.mark.parametrize("k_mode", [1, 3])
+def test_topk_of_the_other_budget_rules(k_mode):
+    B, lens, T = 5, [900, 0, 1, 60, 1000], 128
+    geo = dict(page_tokens=T, n_kv=1, d_h=64, dI=32)
+    table, refs = torch.full((B, 8), -1, dtype=I32, device="cuda"), torch.zeros(1, dtype=I32, device="cuda")
+    pool = torch.zeros(gsa.gsa_cache_page_bytes(gsa.cache_geometry(B=B, n_pages=1, max_pages=1, **geo)), dtype=torch.uint8, device="cuda")
+    c = gsa.make_cache(pool, table, i32(lens), refs, **geo)
+    sc = torch.rand(B, 1, 1000, generator=torch.Generator().manual_seed(5))
+    gp = gsa.make_params(B=B, Lq=1, Lk=1000, n_h=1, n_kv=1, d_h=64, HI=1, dI=32, k_base=50, k_min=5, k_max=1000, v_bar=0.09, k_mode=k_mode)
+    idx, kt = torch.full((B, 1, 1000), -7, dtype=I32, device="cuda"), torch.zeros(B, 1, dtype=I32, device="cuda")
+    ws = torch.empty(gsa.gsa_cache_workspace_bytes(c), dtype=torch.uint8, device="cuda")
+    gsa.gsa_cache_topk(c, gp, sc.cuda(), 1000, idx, kt, None, ws)
+    assert gsa.gsa_device_status(ws) == 0
+    for b, n in enumerate(lens):
+        want, k, _ = (list(range(n)), n, 0.0) if k_mode == 3 else _plain_topk(sc[b, 0].numpy(), n, gp)
+        assert int(kt[b, 0]) == k and idx[b, 0, :k].tolist() == want and (idx[b, 0, k:] == -1).all()
+
+
+def test_workspaces_of_the_size_asked_for_are_enough():
+    """Nothing is written behind the bytes that the size queries name."""
+    geo = GEOMETRIES[2]
+    lens = [500, 40, 0]
+    p = _filled(geo, lens, 45)
+    n = p.ws.numel()
+    guarded = torch.full((n + 65536,), 0x5A, dtype=torch.uint8, device="cuda")
+    p.ws = guarded[:n]
+    p.append([3, 0, 40])
+    # (503 tokens are 16 of 23 pages, 40 are 2: behind the release 5 are free, too few for a copy, enough for one that shares)
+    for call, want in ((lambda: gsa.gsa_cache_fork(p.c, i32([-1, -1, -1]), True, p.ws), 0), (lambda: gsa.gsa_cache_release(p.c, i32([0, 1, 0]), p.ws), 0),
+                       (lambda: gsa.gsa_cache_fork(p.c, i32([-1, 0, -1]), False, p.ws), 7), (lambda: gsa.gsa_cache_compact(p.c, i32([0]), p.ws), 0),
+                       (lambda: gsa.gsa_cache_fork(p.c, i32([-1, 0, -1]), True, p.ws), 0)):
+        call()
+        assert p.status() == want
+    assert (guarded[n:] == 0x5A).all()
+    for Lq, k_max, G in ((1, 16, 8), (1, 400, 8), (39, 400, 1), (3, 37, 4)):
+        gp = gsa.make_params(B=3, Lq=Lq, Lk=500, n_h=2 * G, n_kv=2, d_h=64, HI=2, dI=64, k_base=30, k_min=1, k_max=k_max, v_bar=0.03)
+        n = gsa.gsa_cache_attn_workspace_bytes(gp)
+        guarded = torch.full((n + 65536,), 0x5A, dtype=torch.uint8, device="cuda")
+        Q = torch.randn(3, Lq, 2 * G, 64, generator=p.gen).to(BF16).cuda()
+        idx = torch.randint(0, 40, (3, Lq, k_max), dtype=I32, generator=p.gen).cuda()
+        kt = torch.full((3, Lq), k_max, dtype=I32, device="cuda")
+        gsa.gsa_cache_attn_fwd(p.c, gp, Q, Q, idx, kt, torch.empty_like(Q), guarded[:n])
+        torch.cuda.synchronize()
+        assert (guarded[n:] == 0x5A).all()
+
+
+def test_pages_whose_bytes_lie_behind_four_gigabytes():
+    """The same tokens in a small pool and at the end of one of 5 GB: the same bits from every call."""
+    geo = GEOMETRIES[3]                                                  # 81920 bytes a page
+    lens, n_pages = [700, 300], 60000
+    small = _filled(geo, lens, 46)
+    B, Lq = 2, 1
+    K, V = (torch.zeros(B, 700, 4, 128, dtype=BF16, device="cuda") for _ in range(2))
+    kI = torch.zeros(B, 700, 32, dtype=BF16, device="cuda")
+    gsa.gsa_cache_read(small.c, K, V, kI, small.ws)
+    per = gsa.gsa_cache_page_bytes(small.c)
+    pool = torch.zeros(n_pages * per, dtype=torch.uint8, device="cuda")
+    refs = torch.ones(n_pages, dtype=I32, device="cuda")
+    refs[-40:] = 0
+    assert (n_pages - 40) * per > 1 << 32
+    table, lens_ = torch.full((B, 6), -1, dtype=I32, device="cuda"), torch.zeros(B, dtype=I32, device="cuda")
+    c = gsa.make_cache(pool, table, lens_, refs, page_tokens=128, n_kv=4, d_h=128, dI=32)
+    ws = torch.empty(gsa.gsa_cache_workspace_bytes(c), dtype=torch.uint8, device="cuda")
+    start = torch.zeros(B, dtype=I32, device="cuda")
+    gsa.gsa_cache_reserve(c, i32(lens), start, ws)
+    gsa.gsa_cache_append(c, K, V, None, kI, i32(lens), start, ws)        # (what was read is stored without loss)
+    assert gsa.gsa_device_status(ws) == 0 and int(table.max()) >= n_pages - 40 and int(table[0, 0]) == n_pages - 40
+    gp = gsa.make_params(B=B, Lq=Lq, Lk=700, n_h=8, n_kv=4, d_h=128, HI=4, dI=32, k_base=200, k_min=10, k_max=400, v_bar=0.03)
+    r = lambda *s: torch.randn(*s, generator=small.gen).to(BF16).cuda()  # noqa: E731
+    qI, w, Q, g1 = r(B, 1, 4, 32), torch.rand(B, 1, 4, generator=small.gen).cuda(), r(B, 1, 8, 128), r(B, 1, 8, 128)
+    got = []
+    for cache, w_ in ((small.c, small.ws), (c, ws)):
+        K2, V2, k2 = torch.zeros_like(K), torch.zeros_like(V), torch.zeros_like(kI)
+        gsa.gsa_cache_read(cache, K2, V2, k2, w_)
+        sc = torch.zeros(B, 1, 704, device="cuda")
+        gsa.gsa_cache_indexer_scores(cache, gp, qI, w, None, sc, 704, w_)
+        idx, kt = torch.zeros(B, 1, 400, dtype=I32, device="cuda"), torch.zeros(B, 1, dtype=I32, device="cuda")
+        gsa.gsa_cache_topk(cache, gp, sc, 704, idx, kt, None, w_)
+        out, wa = torch.zeros_like(Q), torch.empty(gsa.gsa_cache_attn_workspace_bytes(gp), dtype=torch.uint8, device="cuda")
+        gsa.gsa_cache_attn_fwd(cache, gp, Q, g1, idx, kt, out, wa)
+        assert gsa.gsa_device_status(wa) == 0
+        got.append((K2, V2, k2, sc, idx, kt, out))
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and torch.equal(got[0][0], K) and (got[0][5] > 0).all()
+    # a copy of a page there, and its way to the front
+    gsa.gsa_cache_release(c, i32([0, 1]), ws)
+    gsa.gsa_cache_fork(c, i32([-1, 0]), False, ws)
+    assert gsa.gsa_device_status(ws) == 0
+    K2 = torch.zeros_like(K)
+    gsa.gsa_cache_read(c, K2, None, None, ws)
+    assert torch.equal(K2[1], K2[0]) and torch.equal(K2[0], K[0])
+    refs[:100] = 0
+    live = torch.zeros(1, dtype=I32, device="cuda")
+    gsa.gsa_cache_compact(c, live, ws)
+    assert gsa.gsa_device_status(ws) == 0 and int(live) == n_pages - 40 - 100 + 12 and int(table.max()) < 100
+    gsa.gsa_cache_read(c, K2, None, None, ws)
+    assert torch.equal(K2[1], K2[0]) and torch.equal(K2[0], K[0])
+
+
 # ---- as it is used -----------------------------------------------------------------------------------------------------------
 def _step(p, gp, x, buf):
     """One decode step: new tokens in, scores, sets, attention."""
