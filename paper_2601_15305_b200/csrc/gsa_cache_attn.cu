@@ -243,6 +243,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
     constexpr int BT = block_tiles(NKV), KPW = BT * kTile / NKV, STEPS = (KPW + 31) / 32;      // keys of a block that a warp looks up
     constexpr bool COLS = G <= 4;          // groups in columns of their own
     constexpr int SETS = G == 4 ? 2 : 1;   // MMAs that the four slots take
+    // Scores that a lane ends up with: keys gid and gid + 8 for two heads, 2 tig, + 1 of eight or 2 (tig & 1), + 1 of four; up to two heads
+    // (a fourth of the exponentials, half of the shuffles: 32 x 128K 31.2 -> 30.3 us; four heads are 2 % slower with two scores
+    // a lane) key gid + 8 (tig >> 1) for head tig & 1, or the one.
+    constexpr bool ONE = G <= 2;
+    constexpr int NH = ONE ? 1 : 2, NS = ONE ? 1 : 4;      // heads and scores
+    constexpr int SPREAD = ONE ? 2 : 4;                    // the lowest bit of the lane numbers that have a head's other keys
     extern __shared__ __align__(16) unsigned char smem[];  // scales, record addresses, rings, cum[rows + 1], budget[rows]
     __shared__ int32_t warp_sum[kWarps];
     __shared__ int32_t cta_bad;
@@ -409,7 +415,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
         uint32_t qz[QPAIR ? KW : 1][4];
         float q_start[SETS][KS][2];        // COLS: what the accumulators start from, -8 times the group's sum of Q
         float q_scale = a.scale_log2;
-        float o[MT][4], m_run[2], l_run[2];
+        float o[MT][4], m_run[NH], l_run[NH];
         int32_t row_first = cum[row], row_end = cum[row + 1], row_k = budget[row];
         auto start_row = [&]() {           // Q into its operand registers, an empty state
             if constexpr (!COLS) {
@@ -473,8 +479,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
             }
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) o[mt][0] = o[mt][1] = o[mt][2] = o[mt][3] = 0.f;
-            m_run[0] = m_run[1] = -INFINITY;
-            l_run[0] = l_run[1] = 0.f;
+#pragma unroll
+            for (int e = 0; e < NH; ++e) { m_run[e] = -INFINITY; l_run[e] = 0.f; }
         };
         // S^T = K Q^T of the tile in stage `st`, in two steps: the products, and what the scales and slots make of them
         constexpr int ACCS = COLS ? SETS * KS : 2;
@@ -532,10 +538,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
                 }
             }
         };
-        auto scale_up = [&](uint32_t st, const float(&acc)[ACCS][4], float(&s)[4]) {
+        auto scale_up = [&](uint32_t st, const float(&acc)[ACCS][4], float(&s)[NS]) {
             if constexpr (COLS) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[e] = 0.f;
+                float t[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int set = 0; set < SETS; ++set) {
                     const int sl = G == 4 ? 2 * set + (tig >> 1) : tig;
@@ -544,15 +549,21 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
 #pragma unroll
                         for (int gr = 0; gr < KS; ++gr) {
                             const float f = scale_at(st + St::kS + (gid + 8 * e) * St::kSRow + sl * KS + gr);
-                            s[2 * e] = fmaf(acc[set * KS + gr][2 * e], f, s[2 * e]);
-                            s[2 * e + 1] = fmaf(acc[set * KS + gr][2 * e + 1], f, s[2 * e + 1]);
+                            t[2 * e] = fmaf(acc[set * KS + gr][2 * e], f, t[2 * e]);
+                            if (G > 1) t[2 * e + 1] = fmaf(acc[set * KS + gr][2 * e + 1], f, t[2 * e + 1]);
                         }
                     }
                 }
+                // sums over the slots' lanes
+                if constexpr (ONE) {                       // each keeps a part of them: of one key, then of one head
+                    const bool second = tig & 2, odd = tig & 1;
+                    float k0 = second ? t[2] : t[0], k1 = second ? t[3] : t[1];
+                    k0 += __shfl_xor_sync(0xFFFFFFFFu, second ? t[0] : t[2], 2);
+                    if (G == 2) k1 += __shfl_xor_sync(0xFFFFFFFFu, second ? t[1] : t[3], 2);
+                    s[0] = (G == 2 && odd ? k1 : k0) + __shfl_xor_sync(0xFFFFFFFFu, G == 2 && !odd ? k1 : k0, 1);
+                } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (G != 4) s[e] += __shfl_xor_sync(0xFFFFFFFFu, s[e], 1);
-                    s[e] += __shfl_xor_sync(0xFFFFFFFFu, s[e], 2);
+                    for (int e = 0; e < 4; ++e) s[e] = t[e] + __shfl_xor_sync(0xFFFFFFFFu, t[e], 2);
                 }
             } else {
 #pragma unroll
@@ -561,7 +572,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
         };
         auto stage_of = [&](int32_t t) { return ring + (uint32_t)(t & (kStages - 1)) * St::kBytes; };
         start_row();
-        float acc[ACCS][4], s[4];
+        float acc[ACCS][4], s[NS];
         cp_async_wait<kStages - 2>();
         __syncwarp();
         multiply(ring, acc);
@@ -590,41 +601,50 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
             if (row_ends) {
                 const int left = row_k - (lo + i - row_first) * kTile;         // keys of this tile
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    if (gid >= left) s[e] = -INFINITY;
-                    if (gid + 8 >= left) s[2 + e] = -INFINITY;
-                }
+                for (int e = 0; e < NS; ++e)
+                    if (gid + 8 * (ONE ? tig >> 1 : e >> 1) >= left) s[e] = -INFINITY;
             }
-            float p[4];
-            auto numerators = [&]() {
+            float p[NS];
+            auto numerators = [&]() -> float {             // and the largest
+                float most = 0.f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p[e] = ex2(fmaf(s[e], q_scale, -m_run[e & 1]));
+                for (int e = 0; e < NS; ++e) {
+                    p[e] = ex2(fmaf(s[e], q_scale, -m_run[e & (NH - 1)]));
+                    most = fmaxf(most, p[e]);
+                }
+                return most;
             };
-            numerators();
-            if (__any_sync(0xFFFFFFFFu, fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])) > kMostNumerator)) {
-                float alpha[2];
+            if (__any_sync(0xFFFFFFFFu, numerators() > kMostNumerator)) {
+                float alpha[NH];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float mx = fmaxf(s[e], s[2 + e]);
-                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
+                for (int e = 0; e < NH; ++e) {
+                    float mx = ONE ? s[e] : fmaxf(s[e], s[e + NS - NH]);
+#pragma unroll
+                    for (int x = SPREAD; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
                     const float m_new = fmaxf(m_run[e], fmaf(mx, q_scale, -kRefUnder));
                     alpha[e] = ex2(m_run[e] - m_new);
                     m_run[e] = m_new;
                     l_run[e] *= alpha[e];
                 }
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    o[mt][0] *= alpha[0]; o[mt][1] *= alpha[1]; o[mt][2] *= alpha[0]; o[mt][3] *= alpha[1];
-                }
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int e = 0; e < NH; ++e) { o[mt][e] *= alpha[e]; o[mt][2 + e] *= alpha[e]; }
                 numerators();
             }
-            l_run[0] += p[0] + p[2];
-            l_run[1] += p[1] + p[3];
-            // (with groups in columns every lane of a key has its scores; the columns of P are those of the heads that there are)
-            const bool head_cols = !COLS || 2 * tig < G;
-            const uint32_t pb0 = transposed(head_cols ? pack_f16(p[0], p[1]) : 0u), pb1 = transposed(head_cols ? pack_f16(p[2], p[3]) : 0u);
+#pragma unroll
+            for (int e = 0; e < NS; ++e) l_run[e & (NH - 1)] += p[e];
+            // P^T's columns: those of the heads that there are.  With one score a lane the matrix turned over has the heads in columns 0 and 2,
+            // and keys 8 to 15 in 4 and 6, which the second operand register has to have in 0 and 2; what the others of O sum up is nothing.
+            uint32_t pb0, pb1;
+            if constexpr (ONE) {
+                pb0 = transposed(pack_f16(p[0], 0.f));
+                pb1 = __shfl_xor_sync(0xFFFFFFFFu, pb0, 16);
+            } else {
+                const bool real = 2 * tig < G;             // (with groups in columns the others have copies)
+                pb0 = transposed(real ? pack_f16(p[0], p[NS - 3]) : 0u);
+                pb1 = transposed(real ? pack_f16(p[NS - 2], p[NS - 1]) : 0u);
+            }
 
             // ---- O^T += V'^T P^T ----
             {
@@ -658,19 +678,18 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
                     do ++next_row; while (cum[next_row + 1] <= row_end);           // (rows with an empty set are passed over)
                     load_q(next_row);
                 }
-                float l[2];
+                float l[NH];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
+                for (int e = 0; e < NH; ++e) {
                     l[e] = l_run[e];
-                    l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 4);
-                    l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 8);
-                    l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 16);
+#pragma unroll
+                    for (int x = SPREAD; x < 32; x <<= 1) l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], x);
                 }
                 const bool whole = row_first >= lo && row_end <= lo + n;
                 const int32_t part = 2 * unit + (row_first > lo ? 1 : 0);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int head = 2 * tig + e;
+                for (int e = 0; e < NH; ++e) {
+                    const int head = NH * tig + e;
                     if (head < G) {
                         float v[DL];
 #pragma unroll
