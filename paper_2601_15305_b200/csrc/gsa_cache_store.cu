@@ -5,7 +5,9 @@
 // present ones are worked on.  (With every thread looking up its own token the read kernel had 275 instructions a thread, the
 // decoding being 70 of them; with a CTA doing it through shared memory its barriers cost as much.)
 // Both kernels stream: HBM bounds them (append: 6 bytes a value of K and V in, 1.1 out; read: 1.1 in, 4 out), next to it, in the append,
-// the sigmoids and the rounding.
+// the sigmoids and the rounding.  8192 tokens of 8 KV heads of 128: append 18.4 us (62 MB: 3.4 TB/s; some 590 instructions for a lane's
+// 48 values, 59 % of the cycles issue one; five, six or eight CTAs an SM without the loads ahead take 1 to 6 % longer), 12291 read
+// back 13 us (67 MB, 5.2 TB/s).
 #include "gsa_cache.cuh"
 
 namespace gsa {
