@@ -327,29 +327,33 @@ def gsa_profile_set_events(ev_begin=None, ev_selected=None, ev_end=None) -> None
 
 
 # ---- the paged 4-bit cache ------------------------------------------------------------------------------------------
-# A decode step makes five of these calls: their arguments are checked with as little work on the host as that takes, and they go
-# through an extension of their own (csrc/gsa_call.c).
+# A decode step makes five of these calls: their arguments are checked, and the library is called, by an extension (csrc/gsa_call.cpp).
 class gsa_cache_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("pool", "table", "lens", "refs")] + \
                [(n, ctypes.c_int32) for n in ("n_pages", "page_tokens", "max_pages", "B", "n_kv", "d_h", "dI")]
 
 
-_call = None
-_addresses = {}
+_CALLS = ("reserve", "append", "read", "fork", "release", "compact", "indexer_scores", "topk", "attn_fwd")     # as bind() takes them
+_call = _ext = None
 
 
 def _address(name: str) -> int:
-    """Where the library's function is; loads the extension that calls it (built with the library)."""
-    global _call
-    if _call is None:
-        lib()
+    """Where the library's function is; loads the extension (built with the library) at the first use."""
+    _extension()
+    return ctypes.cast(getattr(lib(), name), ctypes.c_void_p).value
+
+
+def _extension():
+    global _call, _ext
+    if _ext is None:
+        at = lambda n: ctypes.cast(getattr(lib(), n), ctypes.c_void_p).value  # noqa: E731
         try:
-            from ._gsa_call import call
+            from . import _gsa_call as ext
         except ImportError as e:
             raise GsaError(f"{e}: build it with `python -m paper_2601_15305_b200.build`") from e
-        _call = call
-    a = _addresses[name] = ctypes.cast(getattr(lib(), name), ctypes.c_void_p).value
-    return a
+        ext.bind(GsaError, *[at("gsa_cache_" + n) for n in _CALLS])
+        _call, _ext = ext.call, ext
+    return _ext
 
 
 def cache_geometry(*, B: int, n_pages: int, page_tokens: int, max_pages: int, n_kv: int, d_h: int, dI: int) -> gsa_cache_t:
@@ -372,24 +376,8 @@ def make_cache(pool, table, lens, refs, *, page_tokens: int, n_kv: int, d_h: int
     return c
 
 
-def _at(t, dtype, shape, device: int):
-    """Address of a contiguous tensor of that type and shape on that device; None for None."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
-        raise GsaError(f"expected a contiguous {dtype} tensor {tuple(shape)} on GPU {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
-
-
-def _cache_call(name: str, c: gsa_cache_t, ws, stream, *args) -> None:
-    if torch.cuda.current_device() != c.device or ws.get_device() != c.device or not ws.is_contiguous():
-        raise GsaError("the cache, a contiguous workspace and the current device belong together")
-    # (torch.cuda.current_stream() makes an object: 3 us, a fifth of a call)
-    st = torch._C._cuda_getCurrentRawStream(c.device) if stream is None else stream.cuda_stream
-    at = _addresses.get(name) or _address(name)
-    rc = _call(at, ctypes.addressof(c), *args, ws.data_ptr(), ws.nbytes, st)
-    if rc:
-        _check(rc, name)
+def _raw(stream) -> Optional[int]:
+    return None if stream is None else stream.cuda_stream
 
 
 def gsa_cache_page_bytes(c: gsa_cache_t) -> int:
@@ -412,59 +400,59 @@ def gsa_cache_attn_workspace_bytes(p: gsa_params_t) -> int:
 
 def gsa_cache_reserve(c, n_new, start, ws, stream=None) -> None:
     """Pages for n_new[b] more tokens of every sequence; start[b] receives where they go (-1: refused, see gsa_device_status)."""
-    _cache_call("gsa_cache_reserve", c, ws, stream, _at(n_new, I32, (c.B,), c.device), _at(start, I32, (c.B,), c.device))
+    rc = (_ext or _extension()).reserve(ctypes.addressof(c), c.device, n_new, start, ws, _raw(stream))
+    if rc:
+        _check(rc, "gsa_cache_reserve")
 
 
 def gsa_cache_append(c, K, V, g2, kI, n_new, start, ws, stream=None) -> None:
     """Row i < n_new[b] of K, V * sigmoid(g2) and kI to position start[b] + i of sequence b (g2 None: V already gated)."""
-    if kI is None or kI.dim() != 3:
-        raise GsaError("kI is [B, L_new, dI]")
-    d, B, L = c.device, c.B, kI.shape[1]
-    kv = (B, L, c.n_kv, c.d_h)
-    _cache_call("gsa_cache_append", c, ws, stream, L, _at(K, BF16, kv, d), _at(V, BF16, kv, d), _at(g2, BF16, kv, d),
-                _at(kI, BF16, (B, L, c.dI), d), _at(n_new, I32, (B,), d), _at(start, I32, (B,), d))
+    rc = (_ext or _extension()).append(ctypes.addressof(c), c.device, K, V, g2, kI, n_new, start, ws, _raw(stream))
+    if rc:
+        _check(rc, "gsa_cache_append")
 
 
 def gsa_cache_read(c, K, V, kI, ws, stream=None) -> None:
     """The cache as contiguous tensors [B, L, ...]; any of the three may be None; positions behind a sequence's end stay as they were."""
-    some = next((t for t in (K, V, kI) if t is not None), None)
-    if some is None or some.dim() < 2:
-        raise GsaError("K and V are [B, L, n_kv, d_h], kI [B, L, dI]; at least one of them is wanted")
-    L = some.shape[1]
-    kv = (c.B, L, c.n_kv, c.d_h)
-    _cache_call("gsa_cache_read", c, ws, stream, L, _at(K, BF16, kv, c.device), _at(V, BF16, kv, c.device),
-                _at(kI, BF16, (c.B, L, c.dI), c.device))
+    rc = (_ext or _extension()).read(ctypes.addressof(c), c.device, K, V, kI, ws, _raw(stream))
+    if rc:
+        _check(rc, "gsa_cache_read")
 
 
 def gsa_cache_fork(c, src_of, share: bool, ws, stream=None) -> None:
     """Sequence b becomes a copy of sequence src_of[b] (negative: stays); share: full pages are shared instead of copied."""
-    _cache_call("gsa_cache_fork", c, ws, stream, _at(src_of, I32, (c.B,), c.device), 1 if share else 0)
+    rc = (_ext or _extension()).fork(ctypes.addressof(c), c.device, src_of, 1 if share else 0, ws, _raw(stream))
+    if rc:
+        _check(rc, "gsa_cache_fork")
 
 
 def gsa_cache_release(c, drop, ws, stream=None) -> None:
     """Ends every sequence b with drop[b] != 0."""
-    _cache_call("gsa_cache_release", c, ws, stream, _at(drop, I32, (c.B,), c.device))
+    rc = (_ext or _extension()).release(ctypes.addressof(c), c.device, drop, ws, _raw(stream))
+    if rc:
+        _check(rc, "gsa_cache_release")
 
 
 def gsa_cache_compact(c, live_pages, ws, stream=None) -> None:
     """Moves the live pages to the pool's front; live_pages (one int32) receives their number."""
-    _cache_call("gsa_cache_compact", c, ws, stream, _at(live_pages, I32, (1,), c.device))
+    rc = (_ext or _extension()).compact(ctypes.addressof(c), c.device, live_pages, ws, _raw(stream))
+    if rc:
+        _check(rc, "gsa_cache_compact")
 
 
 def gsa_cache_indexer_scores(c, p, qI, w, bI, scores, row_stride: int, ws, stream=None) -> None:
-    d, B, Lq, HI = c.device, p.B, p.Lq, p.HI
-    _cache_call("gsa_cache_indexer_scores", c, ws, stream, ctypes.addressof(p), _at(qI, BF16, (B, Lq, HI, p.dI), d),
-                _at(w, F32, (B, Lq, HI), d), _at(bI, F32, (HI,), d), _at(scores, F32, (B, Lq, row_stride), d), int(row_stride))
+    rc = (_ext or _extension()).indexer_scores(ctypes.addressof(c), c.device, ctypes.addressof(p), qI, w, bI, scores, row_stride, ws, _raw(stream))
+    if rc:
+        _check(rc, "gsa_cache_indexer_scores")
 
 
 def gsa_cache_topk(c, p, scores, row_stride: int, idx, kt, var, ws, stream=None) -> None:
-    d, rows = c.device, (p.B, p.Lq)
-    _cache_call("gsa_cache_topk", c, ws, stream, ctypes.addressof(p), _at(scores, F32, rows + (row_stride,), d), int(row_stride),
-                _at(idx, I32, rows + (p.k_max,), d), _at(kt, I32, rows, d), _at(var, F32, rows, d))
+    rc = (_ext or _extension()).topk(ctypes.addressof(c), c.device, ctypes.addressof(p), scores, row_stride, idx, kt, var, ws, _raw(stream))
+    if rc:
+        _check(rc, "gsa_cache_topk")
 
 
 def gsa_cache_attn_fwd(c, p, Q, g1, idx, kt, out, ws, stream=None) -> None:
-    d, rows = c.device, (p.B, p.Lq)
-    heads = rows + (p.n_h, p.d_h)
-    _cache_call("gsa_cache_attn_fwd", c, ws, stream, ctypes.addressof(p), _at(Q, BF16, heads, d), _at(g1, BF16, heads, d),
-                _at(idx, I32, rows + (p.k_max,), d), _at(kt, I32, rows, d), _at(out, BF16, heads, d))
+    rc = (_ext or _extension()).attn_fwd(ctypes.addressof(c), c.device, ctypes.addressof(p), Q, g1, idx, kt, out, ws, _raw(stream))
+    if rc:
+        _check(rc, "gsa_cache_attn_fwd")

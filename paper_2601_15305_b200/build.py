@@ -7,13 +7,15 @@ import subprocess
 import sys
 import sysconfig
 
+import torch
+
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 CSRC = os.path.join(_PKG, "csrc")
 LIB_PATH = os.path.join(_PKG, "libgsa_b200.so")
 CALL_PATH = os.path.join(_PKG, "_gsa_call" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-CC = os.environ.get("CC", "gcc")
+CXX = os.environ.get("CXX", "g++")
 
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
          "--expt-relaxed-constexpr", "-Xcompiler", "-fPIC", "-I", os.path.join(_ROOT, "include"), "-I", CSRC]
@@ -27,8 +29,19 @@ def _stale() -> bool:
     if not os.path.exists(LIB_PATH) or not os.path.exists(CALL_PATH):
         return True
     t = min(os.path.getmtime(LIB_PATH), os.path.getmtime(CALL_PATH))
-    deps = sources() + [os.path.join(CSRC, "gsa_call.c")] + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(_ROOT, "include", "*.h"))
+    deps = sources() + [os.path.join(CSRC, "gsa_call.cpp")] + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(_ROOT, "include", "*.h"))
     return any(os.path.getmtime(d) > t for d in deps)
+
+
+def _call_command(out: str) -> list:
+    """Compiles the extension against the installed PyTorch, whose libraries are loaded by the time it is."""
+    t = os.path.dirname(torch.__file__)
+    cuda = os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include")
+    inc = [sysconfig.get_paths()["include"], os.path.join(t, "include"), os.path.join(t, "include", "torch", "csrc", "api", "include"), cuda,
+           os.path.join(_ROOT, "include")]
+    return [CXX, "-O2", "-std=c++17", "-shared", "-fPIC", "-w", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+            *[x for i in inc for x in ("-I", i)], os.path.join(CSRC, "gsa_call.cpp"), "-o", out,
+            "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda"]
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -43,18 +56,19 @@ def build(force: bool = False, verbose: bool = False) -> str:
         objs.append(obj)
         cmd = [NVCC, *FLAGS, "-c", src, "-o", obj] + (["-Xptxas", "-v"] if verbose else [])
         procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    call = CALL_PATH + f".tmp{os.getpid()}"
+    cmd = _call_command(call)
+    procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     for cmd, pr in procs:
         out, _ = pr.communicate()
         if verbose or pr.returncode:
             sys.stderr.write(out)
         if pr.returncode:
-            raise RuntimeError("nvcc failed: " + " ".join(cmd))
+            raise RuntimeError("failed: " + " ".join(cmd))
     tmp = LIB_PATH + f".tmp{os.getpid()}"
     subprocess.check_call([NVCC, "-shared", "-o", tmp, *objs, "-lcudart", "-ldl"])
     os.replace(tmp, LIB_PATH)
-    tmp = CALL_PATH + f".tmp{os.getpid()}"
-    subprocess.check_call([CC, "-O2", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "gsa_call.c"), "-o", tmp])
-    os.replace(tmp, CALL_PATH)
+    os.replace(call, CALL_PATH)
     return LIB_PATH
 
 

@@ -943,3 +943,58 @@ def test_chunked_prefill_reads_the_cache_back():
     for t in range(0, Lq, 7):
         want, mag = p.plain.attn(0, f64(Q[0, t]), f64(g1[0, t]), sets[0][t], 128 ** -0.5)
         assert (np.abs(f64(out[0, t]) - f64(out4[0, t])) <= 2 * 2.0 ** -8 * (mag + np.abs(want)) * 1.05 + 1e-6).all()
+
+
+def test_binding_refuses_tensors_that_do_not_fit():
+    geo = GEOMETRIES[2]
+    p = _filled(geo, [100, 60], 47)
+    c, ws = p.c, p.ws
+    gp = gsa.make_params(B=2, Lq=1, Lk=100, n_h=4, n_kv=2, d_h=64, HI=2, dI=64, k_base=8, k_min=1, k_max=16)
+    new = lambda *s, dtype=BF16: torch.zeros(*s, dtype=dtype, device="cuda")  # noqa: E731
+    n2, kv, k3 = new(2, dtype=I32), new(2, 3, 2, 64), new(2, 3, 64)
+    good = {
+        "gsa_cache_reserve": [n2, new(2, dtype=I32)], "gsa_cache_append": [kv, kv, kv, k3, n2, n2], "gsa_cache_read": [kv, kv, k3],
+        "gsa_cache_release": [n2], "gsa_cache_compact": [new(1, dtype=I32)],
+        "gsa_cache_indexer_scores": [gp, new(2, 1, 2, 64), new(2, 1, 2, dtype=F32), new(2, dtype=F32), new(2, 1, 100, dtype=F32), 100],
+        "gsa_cache_topk": [gp, new(2, 1, 100, dtype=F32), 100, new(2, 1, 16, dtype=I32), new(2, 1, dtype=I32), new(2, 1, dtype=F32)],
+        "gsa_cache_attn_fwd": [gp, new(2, 1, 4, 64), new(2, 1, 4, 64), new(2, 1, 16, dtype=I32), new(2, 1, dtype=I32), new(2, 1, 4, 64)],
+    }
+    n0, before = gsa.gsa_launch_count(), p.lens.clone()
+    for name, args in good.items():
+        f = getattr(gsa, name)
+        for i, a in enumerate(args):
+            if not isinstance(a, torch.Tensor):
+                continue
+            wide = torch.zeros(tuple(a.shape) + (2,), dtype=a.dtype, device="cuda")[..., 0]        # the right shape, strided
+            others = [a.cpu(), a.to(torch.float16), torch.zeros(tuple(a.shape)[:-1] + (a.shape[-1] + 1,), dtype=a.dtype, device="cuda"), [1, 2]]
+            for bad in others + ([wide] if a.numel() > 1 else []):
+                with pytest.raises(gsa.GsaError):
+                    f(c, *args[:i], bad, *args[i + 1:], ws)
+        for bad_ws in (None, ws.cpu(), ws[:8], ws[::2], ws.data_ptr()):
+            with pytest.raises(gsa.GsaError):
+                f(c, *args, bad_ws)
+    with pytest.raises(gsa.GsaError):
+        gsa.gsa_cache_fork(c, n2.float(), True, ws)
+    assert gsa.gsa_launch_count() == n0 and torch.equal(p.lens, before)
+
+
+def test_calls_on_a_stream_that_is_not_the_current_one():
+    geo = GEOMETRIES[0]
+    p = _filled(geo, [300, 200], 48)
+    gp = gsa.make_params(B=2, Lq=1, Lk=320, n_h=16, n_kv=8, d_h=128, HI=8, dI=64, k_base=40, k_min=8, k_max=64, v_bar=0.03)
+    gen = torch.Generator().manual_seed(49)
+    x = {k: v.cuda() for k, v in _step_inputs(p, gp, gen).items()}
+    buf, side = _step_buffers(gp), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    late = torch.zeros(64 << 20, device="cuda")
+    with torch.cuda.stream(side):                                        # work ahead of the step on its stream, none on the current one
+        for _ in range(20):
+            late += 1
+        x["Q"].mul_(0.5)
+    gsa.gsa_cache_reserve(p.c, buf["n_new"], buf["start"], p.ws, stream=side)
+    gsa.gsa_cache_append(p.c, x["K"], x["V"], x["g2"], x["kI"], buf["n_new"], buf["start"], p.ws, stream=side)
+    gsa.gsa_cache_indexer_scores(p.c, gp, x["qI"], x["w"], None, buf["scores"], buf["scores"].shape[-1], p.ws, stream=side)
+    gsa.gsa_cache_topk(p.c, gp, buf["scores"], buf["scores"].shape[-1], buf["idx"], buf["kt"], None, p.ws, stream=side)
+    gsa.gsa_cache_attn_fwd(p.c, gp, x["Q"], x["g1"], buf["idx"], buf["kt"], buf["out"], buf["ws"], stream=side)
+    side.synchronize()
+    _plain_step(p, gp, x, buf)
