@@ -35,7 +35,7 @@
 //
 // Bound: the issue of instructions, some 500 for a tile and KV head, by four warps a scheduler (the registers allow no more; 57 % of all
 // cycles issue one, and most others wait for a fixed latency or the ALU).  32 sequences of 16K to 128K, 16 heads on 8 KV heads of 128: 71 MB of
-// records, 30.3 us with the merge, 2.3 TB/s; some 6 us pass before the first tile (budgets, indices, pages, records: four loads in a
+// records, 30.0 us with the merge, 2.4 TB/s; some 6 us pass before the first tile (budgets, indices, pages, records: four loads in a
 // row), 18 us in the loop, 6 us from its end to the end of the merge.  257 rows of 1000 of 20011 keys, 32 heads on 8 of 64: 60 us.
 // (Four query heads at d_h = 128 spill 88 to 220 bytes a thread.)
 #include "gsa_cache.cuh"
@@ -53,7 +53,7 @@ constexpr int kLut = 256;                  // scales by their byte, as fp32
 constexpr int kMinTiles = 2;               // fewest tiles worth a unit of their own
 constexpr int kMaxSplitRows = 2048;        // rows of one launch, whose budgets a CTA sums up (16 KB of its shared memory)
 constexpr int kAddressBlocks = 4;          // blocks of record addresses: being read, next, being written (and a power of two)
-constexpr int kOwnTiles = 2;               // tiles a unit, at most, for rows with a CTA of their own; twice as many if they occupy half the SMs
+constexpr int kOwnTiles = 1, kManyOwnTiles = 4;        // tiles a unit, at most, for rows with a CTA of their own; the same if they occupy half the SMs
 constexpr int kMergeWarps = 8;
 constexpr float kRefUnder = 7.0f;          // a new softmax reference lies 2^7 under the score that moved it there,
 constexpr float kMostNumerator = 32768.0f; // and moves again when a score lies 2^15 above it (fp16 ends at 2^16)
@@ -937,10 +937,10 @@ cudaError_t launch_cache_attn(const CacheView& c, const gsa_params_t& p, const _
     char* s = (char*)ws + kStatusBytes;
     a.status = ws; a.state = (float*)s; a.stats = (float2*)(s + w.stats); a.merges = (int4*)(s + w.merges); a.flags = (int32_t*)(s + w.flags);
     const int32_t all = p.B * p.Lq, subs = kWarps / p.n_kv;
-    // A CTA for each row, or equal runs and a merge?  Measured (us, sets of k keys; own CTA / runs):  8 KV heads of 128, up to 32 rows: k 32
-    // 7.8 / 8.8, 64 9.5 / 9.1, 128 12.8 / 9.2;  128 rows: 64 9.9 / 11.9, 256 18.5 / 21.4;  one of 64, up to 32 rows: 256 7.0 / 7.5, 512 8.4 /
-    // 7.6;  two of 128, 128 rows: 256 11.1 / 16.9.  The launch that runs take more costs the host 2.4 us; rows of unequal sets favour runs.
-    if (all <= sm_count() && (p.k_max + kTile - 1) / kTile <= (2 * all >= sm_count() ? 2 : 1) * kOwnTiles * subs) {
+    // A CTA for each row, or equal runs and a merge?  A tile takes some 1.5 us where all sixteen warps of an SM have one, the merge 2 to 4.
+    // Measured (us in a graph, sets of k keys; own CTA / runs), up to 32 rows: 8 KV heads of 128, k 32 7.0 / 8.8, 64 9.1 / 8.4; two of 128, 128
+    // 7.9 / 8.4, 256 10.9 / 8.0; one of 64, 256 6.8 / 7.5, 512 8.3 / 7.2;  128 rows: 8 of 128, 64 9.9 / 11.9; two of 128, 256 11.1 / 16.9.
+    if (all <= sm_count() && (p.k_max + kTile - 1) / kTile <= (2 * all >= sm_count() ? kManyOwnTiles : kOwnTiles) * subs) {
         a.own = 1; a.rows = all;
         a.Q = Q; a.g1 = g1; a.out = out; a.idx = idx; a.kt = kt;
         return p.d_h == 128 ? launch_groups<128>(a, st) : launch_groups<64>(a, st);

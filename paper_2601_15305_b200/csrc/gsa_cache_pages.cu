@@ -5,7 +5,7 @@
 // the r-th free page goes to the r-th request, requests in the order of the sequences.  So the outcome depends on nothing but the
 // tables, and a call that does not fit is refused before it has changed anything.  Bound: latency of the reads of the counts (65536 of
 // them are 256 KB for one SM); a call that takes no page does not read them.  Page copies are a second kernel over the whole GPU, bound
-// by HBM (every byte read and written once).  Eight prompts to 32 beams and their release: 15 us, three launches of 4 to 8 (counts asked
+// by HBM (every byte read and written once).  Eight prompts to 32 beams and their release: 13 us, three launches (counts asked
 // for together with the lengths changed nothing); 5600 pages of 80 KB of which a fourth move: 6 us of plan, 35 of copies.
 #include "gsa_cache.cuh"
 

@@ -612,12 +612,12 @@ def test_attention_of_large_sets_of_every_head_layout(geo, G):
 
 
 @pytest.mark.parametrize("rows", [30, 73, 74, 148, 149])
-@pytest.mark.parametrize("k_max", [64, 65, 128, 129])
+@pytest.mark.parametrize("k_max", [32, 33, 64, 65, 128, 129])
 def test_attention_on_both_sides_of_the_row_split(rows, k_max):
-    """Eight KV heads: two units a CTA, so that sets of 64 keys (128, where rows fill half the SMs) end the form with a CTA for each row."""
+    """Eight KV heads: two units a CTA, so that sets of 32 keys (128, where rows fill half the SMs) end the form with a CTA for each row."""
     geo = GEOMETRIES[5]
     p = _filled(geo, [rows + 150], 41)
-    sets = _random_sets(np.random.default_rng(k_max), [rows + 150], rows, [k_max, k_max, 1, 0, k_max - 15, 33])
+    sets = _random_sets(np.random.default_rng(k_max), [rows + 150], rows, [k_max, k_max, 1, 0, k_max - 15, min(k_max, 33)])
     Q, g1, out, status, _ = _attend(p, 2, rows, sets, k_max)
     assert status == 0
     _check_rows(p, Q, g1, out, sets, rows, 64 ** -0.5, rows={(0, t) for t in list(range(0, rows, 11)) + [rows - 2, rows - 1]})
