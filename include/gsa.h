@@ -400,6 +400,8 @@ int gsa_cache_workspace_bytes(const gsa_cache_t *c, size_t *bytes);
  * Pages for n_new[b] more tokens of every sequence: start[b] = lens[b], lens[b] += n_new[b], free pages taken lowest number
  * first, in the order of the sequences.  All or nothing: if the pool has too few free pages, a table row is too short, or an
  * n_new is negative, nothing changes, every start[b] is -1 (gsa_cache_append then writes nothing) and the status word says so.
+ * A gsa_cache_append behind it on the same workspace keeps that report, every other call on it writes its own: a step that is
+ * enqueued whole gives its stages another workspace, and looks at both.
  *   n_new, start  [B] int32 on the device, distinct
  */
 int gsa_cache_reserve(const gsa_cache_t *c, const int32_t *n_new, int32_t *start, void *ws, size_t ws_bytes, void *stream);
@@ -412,7 +414,8 @@ int gsa_cache_reserve(const gsa_cache_t *c, const int32_t *n_new, int32_t *start
  *                   taken as already gated
  *   n_new, start    [B] int32 on the device, as given to and written by gsa_cache_reserve; rows i >= n_new[b] are not
  *                   read, and a sequence with start[b] < 0 is left out; an n_new[b] above L_new is reported
- * A position outside [0, lens[b]) or on a page that is shared (refs != 1) is skipped and reported.
+ * A position outside [0, lens[b]) or on a page that is shared (refs != 1) is skipped and reported.  Behind a refused gsa_cache_reserve
+ * on the same workspace, an n_new[b] > 0 whose start[b] is negative is reported as that call reported it.
  */
 int gsa_cache_append(const gsa_cache_t *c, int32_t L_new, const void *K, const void *V, const void *g2_logits, const void *kI,
                      const int32_t *n_new, const int32_t *start, void *ws, size_t ws_bytes, void *stream);
@@ -428,7 +431,9 @@ int gsa_cache_read(const gsa_cache_t *c, int32_t L, void *K, void *V, void *kI, 
  * Sequence b becomes a copy of sequence src_of[b] (negative: b stays as it is).  With share != 0 its full pages are shared
  * and the partly filled last one is copied; otherwise every page is copied.  New pages are taken lowest number first, in the
  * order of the sequences.  All or nothing, as gsa_cache_reserve: refused if pages are missing, if lens[b] != 0, if src_of[b]
- * is not a sequence or is itself a copy of this call.
+ * is not a sequence or is itself a copy of this call.  A refusal leaves the copies' lengths 0: a gsa_cache_release of the
+ * sources that is enqueued behind it, before anybody has looked at the status, takes its drop from those lengths on the device,
+ * or the sources are lost with the copies.
  *   src_of  [B] int32 on the device
  */
 int gsa_cache_fork(const gsa_cache_t *c, const int32_t *src_of, int32_t share, void *ws, size_t ws_bytes, void *stream);
@@ -475,7 +480,7 @@ int gsa_cache_attn_fwd(const gsa_cache_t *c, const gsa_params_t *p, const void *
  * Waits for `stream`, reads the device status word at the start of `ws` (a gsa_cache_* call's, and the words behind it) into
  * *status_out (host) and returns GSA_OK, GSA_ERR_DEVICE_TIMEOUT (*status_out 1..3: copy producer,
  * MMA issuer, epilogue), GSA_ERR_INDEX_RANGE (*status_out 6) or GSA_ERR_CACHE_FULL (*status_out 7) accordingly.
- * The word is cleared by every call that takes `ws`.  ws == NULL reads the status word of
+ * The word is cleared by every call that takes `ws` (gsa_cache_append keeps a refused reservation's).  ws == NULL reads the status word of
  * gsa_sparse_gated_attn_fwd_static (it lives in the library's built-in array on the current device).
  */
 int gsa_device_status(const void *ws, void *stream, int32_t *status_out);

@@ -42,14 +42,19 @@ __device__ __forceinline__ int32_t checked_page(const CacheView& c, int32_t b, i
 // after its first (`before` != 0) add to the words.
 constexpr int kFlagsWord = 10;             // int32 word of the head: number of words behind it (0: the status word is all there is)
 constexpr int kMaxFlags = 4096;
-__device__ __forceinline__ void write_flags(int32_t* ws, bool bad, int32_t before = 0) {
+// A refused reservation leaves kRefusedMark in this word of the head, next to its status.  The append behind it on the same workspace stores
+// nothing, and would otherwise write "nothing wrong" over the only sign of it: it keeps both (`refused`: the status).
+constexpr int kRefusedWord = 11;
+constexpr int32_t kRefusedMark = 0x52534552;
+__device__ __forceinline__ void write_flags(int32_t* ws, bool bad, int32_t before = 0, int32_t refused = kDevOk) {
     const int any = __syncthreads_or(bad);
     if (threadIdx.x == 0) {
         int32_t* mine = ws + kStatusBytes / 4 + blockIdx.x;
         *mine = (any || (before && *mine)) ? kDevBadIndex : kDevOk;
     }
     if (blockIdx.x == 0 && !before)
-        for (int i = threadIdx.x; i < kStatusBytes / 4; i += blockDim.x) ws[i] = i == kFlagsWord ? (int32_t)gridDim.x : 0;
+        for (int i = threadIdx.x; i < kStatusBytes / 4; i += blockDim.x)
+            ws[i] = i == 0 ? refused : i == kFlagsWord ? (int32_t)gridDim.x : i == kRefusedWord && refused != kDevOk ? kRefusedMark : 0;
 }
 
 // ---- launchers -------------------------------------------------------------------------------------------------------------

@@ -103,9 +103,9 @@ __device__ __forceinline__ int seq_of(const PlanShared& sh, int B, uint32_t r) {
     return lo;
 }
 
-__device__ __forceinline__ void write_head(int32_t* ws, int32_t status, int32_t copies, int32_t live) {
+__device__ __forceinline__ void write_head(int32_t* ws, int32_t status, int32_t copies, int32_t live, int32_t mark = 0) {
     for (int i = threadIdx.x; i < kStatusBytes / 4; i += kPlanThreads)
-        ws[i] = i == 0 ? status : i == kCopiesWord ? copies : i == kLiveWord ? live : 0;
+        ws[i] = i == 0 ? status : i == kCopiesWord ? copies : i == kLiveWord ? live : i == kRefusedWord ? mark : 0;
 }
 
 __device__ __forceinline__ int pages_of(const CacheView& c, int n) { return (n + c.T - 1) >> c.log_t; }
@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(kPlanThreads) gsa_cache_reserve_kernel(const C
             if (status == kDevOk && add[i]) c.lens[b] = len[i] + add[i];
         }
     }
-    write_head(ws, status, 0, 0);
+    write_head(ws, status, 0, 0, status == kDevOk ? 0 : kRefusedMark);
 }
 
 // Plan of a fork: new pages into the tables, the pages to copy into the list (source, destination).

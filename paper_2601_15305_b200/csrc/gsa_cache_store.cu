@@ -232,10 +232,20 @@ __device__ __forceinline__ void each_key_piece(const StoreArgs& a, const Token& 
     }
 }
 
+// What the first CTA of an append has to keep in the head: the status of a reservation that was refused, if tokens were given that it left
+// without a place.  (The mark alone does not tell: the caller may have made places of its own since, or given nothing.)
+__device__ __noinline__ int32_t refused_status(const StoreArgs& a) {
+    const int32_t status = a.ws[0];
+    bool lost = false;
+    for (int b = threadIdx.x; b < a.c.B; b += kStoreThreads) lost |= __ldg(a.start + b) < 0 && __ldg(a.n_new + b) > 0;
+    return __syncthreads_or(lost) && (status == kDevCacheFull || status == kDevBadIndex) ? status : kDevOk;
+}
+
 template <bool GATE>
 __global__ void __launch_bounds__(kStoreThreads, 4) gsa_cache_append_kernel(const StoreArgs a) {
     chain_wait();
     const CacheView& c = a.c;
+    const int32_t mark = blockIdx.x == 0 ? a.ws[kRefusedWord] : 0;
     const int lane = threadIdx.x & 31;
     const int D = c.n_kv * c.d_h, log_head = c.d_h == 128 ? 3 : 2, groups = 1 << a.log_groups;       // groups of a head: 8 or 4
     bool bad = false;
@@ -275,7 +285,7 @@ __global__ void __launch_bounds__(kStoreThreads, 4) gsa_cache_append_kernel(cons
             reinterpret_cast<uint4*>(c.pool + key)[j] = __ldg(reinterpret_cast<const uint4*>(a.kI + token * c.dI) + j);
         });
     }
-    write_flags(a.ws, bad);
+    write_flags(a.ws, bad, 0, mark == kRefusedMark ? refused_status(a) : kDevOk);
 }
 
 __global__ void __launch_bounds__(kStoreThreads, 8) gsa_cache_read_kernel(const StoreArgs a) {
