@@ -458,7 +458,8 @@ int gsa_cache_compact(const gsa_cache_t *c, int32_t *live_pages, void *ws, size_
  * and q_begin / q_end are ignored.
  *
  * gsa_cache_indexer_scores: gsa_indexer_scores with k^I from the cache.  For few rows a sequence (decode): every row reads the
- *   sequence's k^I by itself.  scores [B, Lq, row_stride], written for the visible keys.
+ *   sequence's k^I by itself.  scores [B, Lq, row_stride], written for the visible keys.  A NaN in qI, w or bI makes the scores NaN that
+ *   it belongs to, one in a k^I that key's: gsa_cache_topk puts a NaN above every score.
  * gsa_cache_topk: gsa_adaptive_topk for those rows.  A row that sees no key gets kt = 0 and var = 0.
  * gsa_cache_attn_fwd: gsa_sparse_gated_attn_fwd with K and V' from the cache.  Q, g1_logits, out [B, Lq, n_h, d_h] bf16,
  *   idx [B, Lq, k_max], kt [B, Lq]; the entries of a set may stand in any order.  A row with kt = 0 is written as zeros.

@@ -36,6 +36,18 @@ __device__ __forceinline__ int32_t checked_page(const CacheView& c, int32_t b, i
     return 0;
 }
 
+// The smaller and the larger of two, NaN if one of them is (fminf and fmaxf give the other).  One instruction either way.
+__device__ __forceinline__ float min_nan(float a, float b) {
+    float d;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+
 // What the CTAs of a call found wrong.  Each writes a word of its own behind the head, the first one the head, which says how many there are:
 // gsa_device_status adds them up.  Nothing has to be cleared ahead of the call, which would be a launch of its own (2 us of the GPU, as
 // much of the host).  Called by all threads of every CTA of a one-dimensional grid of at most kMaxFlags; launches of one call

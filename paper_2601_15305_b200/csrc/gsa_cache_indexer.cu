@@ -60,7 +60,7 @@ struct RowQuery {
         }
     }
     // scores of keys gid and gid + 8 of a tile, in every lane of a key
-    __device__ __forceinline__ void score(const KeyTile<DI>& ka, int act, float (&acc)[2]) const {
+    __device__ __forceinline__ void score(const KeyTile<DI>& ka, int act, int tig, float (&acc)[2]) const {
         float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int ks = 0; ks < kElems / 4; ++ks)         // one k-step uses 4 of the lane's elements
@@ -71,11 +71,14 @@ struct RowQuery {
             float v = 0.f;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
+                // A NaN stays one (fminf, fmaxf would make it a gate of 2^-80, a closed ReLU: a key that is never chosen, and nothing to
+                // show for it).  Columns without a head are 0: a key's infinity times their zeros is none of it.
+                const float x = HI == 8 || 2 * tig + e < HI ? s[hf * 2 + e] : 0.f;
                 if (act == 1) {                                     // Eq. 3: ReLU
-                    v = fmaf(wv[e], fmaxf(s[hf * 2 + e] + bv[e], 0.f), v);
+                    v = fmaf(wv[e], max_nan(x + bv[e], 0.f), v);
                 } else {
                     float ex, rc;
-                    const float arg = fminf(fmaf(s[hf * 2 + e], -1.4426950408889634f, bv[e]), 80.f);
+                    const float arg = min_nan(fmaf(x, -1.4426950408889634f, bv[e]), 80.f);
                     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(ex) : "f"(arg));
                     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rc) : "f"(1.0f + ex));
                     v = fmaf(wv[e], rc, v);
@@ -182,7 +185,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) gsa_cache_indexer_kernel(const
 #pragma unroll
             for (int u = 0; u < kStepTiles; ++u) {
                 float acc[2];
-                q.score(ka[u], a.act, acc);
+                q.score(ka[u], a.act, tig, acc);
                 const int32_t key = k0 + u * 16 + (tig & 1) * 8 + gid;
                 if (tig < 2 && key < k_end) out_row[key] = acc[tig & 1];
             }
