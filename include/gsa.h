@@ -466,7 +466,7 @@ int gsa_cache_compact(const gsa_cache_t *c, int32_t *live_pages, void *ws, size_
  *   Sums and softmax statistics are fp32.  For the product with V' the softmax numerators are rounded to fp16, scaled so that a row's
  *   largest lies between 2^7 and 2^15: to 2^-11 of one, or 2^-32 of the row's sum where that is more.  With up to four query heads a KV
  *   head a finite |q| sm_scale of 2^117 and more may count as infinite.  An infinity or NaN in Q, or in a selected K, makes the head's
- *   row NaN, one in a selected V' the 16 values that share its scale.
+ *   row NaN, one in a selected V' the 16 values that share its scale, a NaN in g1_logits its output.
  *   ws: gsa_cache_attn_workspace_bytes(p).  The result does not depend on scheduling.
  */
 int gsa_cache_indexer_scores(const gsa_cache_t *c, const gsa_params_t *p, const void *qI, const float *w, const float *bI,

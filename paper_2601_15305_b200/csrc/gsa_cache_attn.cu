@@ -173,6 +173,13 @@ __device__ __forceinline__ void values_f16x2(uint32_t (&v)[4], uint32_t m, uint3
     }
 }
 
+// fast_sigmoid, but a NaN stays one (there the clamp makes it 2^-126: a row of almost zeros, and nothing to show for it)
+__device__ __forceinline__ float gate_of(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + ex2(min_nan(-1.4426950408889634f * x, 126.f))));
+    return r;
+}
+
 // N results of one head, gated and rounded
 template <int N>
 __device__ __forceinline__ void write_gated(const CacheAttnArgs& a, int64_t at, const float (&o)[N]) {
@@ -185,8 +192,8 @@ __device__ __forceinline__ void write_gated(const CacheAttnArgs& a, int64_t at, 
         uint32_t w[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            w[j] = pack_bf16(o[i * 8 + 2 * j] * fast_sigmoid(__uint_as_float(gw[j] << 16)),
-                             o[i * 8 + 2 * j + 1] * fast_sigmoid(__uint_as_float(gw[j] & 0xFFFF0000u)));
+            w[j] = pack_bf16(o[i * 8 + 2 * j] * gate_of(__uint_as_float(gw[j] << 16)),
+                             o[i * 8 + 2 * j + 1] * gate_of(__uint_as_float(gw[j] & 0xFFFF0000u)));
         to[i] = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
@@ -752,8 +759,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
 #pragma unroll
                 for (int d = 0; d < N; d += 2) {
                     const uint32_t g = __ldg(reinterpret_cast<const uint32_t*>(a.g1 + at) + d / 2);
-                    reinterpret_cast<uint32_t*>(a.out + at)[d / 2] = pack_bf16(o[d] * inv * fast_sigmoid(__uint_as_float(g << 16)),
-                                                                               o[d + 1] * inv * fast_sigmoid(__uint_as_float(g & 0xFFFF0000u)));
+                    reinterpret_cast<uint32_t*>(a.out + at)[d / 2] = pack_bf16(o[d] * inv * gate_of(__uint_as_float(g << 16)),
+                                                                               o[d + 1] * inv * gate_of(__uint_as_float(g & 0xFFFF0000u)));
                 }
             }
         }
@@ -867,7 +874,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) gsa_cache_merge_kernel(const
 #pragma unroll
     for (int d = 0; d < N; d += 2)
         reinterpret_cast<uint32_t*>(a.out + at_out)[d / 2] =
-            pack_bf16(o[d] * inv * fast_sigmoid(__uint_as_float(gate[d / 2] << 16)), o[d + 1] * inv * fast_sigmoid(__uint_as_float(gate[d / 2] & 0xFFFF0000u)));
+            pack_bf16(o[d] * inv * gate_of(__uint_as_float(gate[d / 2] << 16)), o[d + 1] * inv * gate_of(__uint_as_float(gate[d / 2] & 0xFFFF0000u)));
 }
 
 int32_t unit_count(const gsa_params_t& p) { return sm_count() * (kWarps / p.n_kv); }

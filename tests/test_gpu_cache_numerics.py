@@ -1,10 +1,10 @@
-"""Values that the cache's kernels must not lose: NaN and infinities in what the indexer's scores are made of."""
+"""Values that the cache's kernels must not lose: NaN and infinities in queries, keys, biases and gates."""
 import numpy as np
 import pytest
 import torch
 
 from paper_2601_15305_b200 import binding as gsa
-from test_gpu_cache import BF16, GEOMETRIES, I32, _filled, f64
+from test_gpu_cache import BF16, GEOMETRIES, I32, _filled, _random_sets, f64, i32
 
 pytestmark = pytest.mark.gpu
 NAN, INF = float("nan"), float("inf")
@@ -81,3 +81,46 @@ def test_infinities_in_the_scores(HI, act):
         fin = np.isfinite(want)
         # (the terms of a score: 64 products of which the sum is below 64, see the other tests)
         assert np.abs(got[fin] - want[fin]).max(initial=0) <= HI * (72 * 2.0 ** -23 * 64 * (1.0 if act else 0.25) + 2.0 ** -20 + 64 * 2.0 ** -23)
+
+
+def _attention(p, G, Lq, sets, k_max, Q, g1, sm_scale=0.0):
+    P = p.plain
+    idx, kt = np.full((P.B, Lq, k_max), -1, np.int32), np.zeros((P.B, Lq), np.int32)
+    for b in range(P.B):
+        for t in range(Lq):
+            kt[b, t] = len(sets[b][t])
+            idx[b, t, :kt[b, t]] = sets[b][t]
+    gp = gsa.make_params(B=P.B, Lq=Lq, Lk=int(P.lens.max()), n_h=P.n_kv * G, n_kv=P.n_kv, d_h=P.d_h, HI=1, dI=P.dI, k_base=1, k_min=1, k_max=k_max,
+                         sm_scale=sm_scale)
+    out = torch.full((P.B, Lq, P.n_kv * G, P.d_h), -3.0, dtype=BF16, device="cuda")
+    ws = torch.full((gsa.gsa_cache_attn_workspace_bytes(gp),), 0xFF, dtype=torch.uint8, device="cuda")
+    gsa.gsa_cache_attn_fwd(p.c, gp, Q.cuda(), g1.cuda(), i32(idx), i32(kt), out, ws)
+    assert gsa.gsa_device_status(ws) == 0
+    return out
+
+
+@pytest.mark.parametrize("G", [1, 2, 4, 8])
+@pytest.mark.parametrize("geo,sizes,k_max,Lq", [(GEOMETRIES[0], [16, 9], 16, 1), (GEOMETRIES[1], [200, 150], 200, 1), (GEOMETRIES[4], [700, 690], 700, 1),
+                                                (GEOMETRIES[5], [30, 700], 700, 1), (GEOMETRIES[5], [700, 16, 650], 700, 40)])
+def test_a_nan_in_the_output_gate_shows(geo, sizes, k_max, Lq, G):
+    """Rows finished by one unit, by a CTA of their own, and by the merge kernel, with eight warps a row and with one."""
+    lens = [750, 750]
+    p = _filled(geo, lens, 73)
+    sets = _random_sets(np.random.default_rng(G), lens, Lq, sizes)
+    n_h, d = geo["n_kv"] * G, geo["d_h"]
+    gen = torch.Generator().manual_seed(74)
+    Q, g1 = torch.randn(2, Lq, n_h, d, generator=gen).to(BF16), torch.randn(2, Lq, n_h, d, generator=gen).to(BF16)
+    clean = _attention(p, G, Lq, sets, k_max, Q, g1)
+    spoilt, expect = g1.clone(), torch.zeros(g1.shape, dtype=torch.bool)
+    for b in range(2):
+        for t in range(Lq):
+            for h, i in ((0, 0), (n_h - 1, d - 1), (n_h // 2, 17), (0, d - 2)):
+                spoilt[b, t, h, i], expect[b, t, h, i] = NAN, True
+    spoilt[0, 0, 0, 1], spoilt[0, 0, 0, 2] = INF, -INF                   # gates of 1 and 0
+    out = _attention(p, G, Lq, sets, k_max, Q, spoilt).cpu()
+    assert torch.equal(out.isnan(), expect)
+    kept = ~expect
+    kept[0, 0, 0, 1:3] = False
+    assert torch.equal(out[kept], clean.cpu()[kept])
+    want, mag = p.plain.attn(0, f64(Q[0, 0]), np.full((n_h, d), 60.0), np.asarray(sets[0][0]), d ** -0.5)
+    assert abs(float(out[0, 0, 0, 1]) - want[0, 1]) <= 2.0 ** -8 * abs(want[0, 1]) + 2.0 ** -10 * mag[0, 1] and abs(float(out[0, 0, 0, 2])) <= 2.0 ** -100
