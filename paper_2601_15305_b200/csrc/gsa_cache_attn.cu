@@ -55,7 +55,7 @@ constexpr int kMaxSplitRows = 2048;        // rows of one launch, whose budgets 
 constexpr int kAddressBlocks = 4;          // blocks of record addresses: being read, next, being written (and a power of two)
 constexpr int kOwnTiles = 1, kManyOwnTiles = 4;        // tiles a unit, at most, for rows with a CTA of their own; the same if they occupy half the SMs
 constexpr int kMergeWarps = 8;
-constexpr float kRefUnder = 7.0f;          // a new softmax reference lies 2^7 under the score that moved it there,
+constexpr float kRefUnder = 7.0f;          // a new softmax reference lies 2^7 under the score that moved it there (2^0 to 2^14 where fp32 cannot tell),
 constexpr float kMostNumerator = 32768.0f; // and moves again when a score lies 2^15 above it (fp16 ends at 2^16)
 
 struct CacheAttnArgs {
@@ -622,7 +622,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
                 float most = 0.f;
 #pragma unroll
                 for (int e = 0; e < NS; ++e) {
-                    p[e] = ex2(fmaf(s[e], q_scale, -m_run[e & (NH - 1)]));
+                    // (The score is rounded before the reference is taken off: in one multiply-add the difference from a reference near
+                    // 2^28, itself rounded to a multiple of 32, could be anything, and the numerator infinite.)
+                    p[e] = ex2(__fadd_rn(__fmul_rn(s[e], q_scale), -m_run[e & (NH - 1)]));
                     most = fmaxf(most, p[e]);
                 }
                 return most;
@@ -634,7 +636,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
                     float mx = ONE ? s[e] : fmaxf(s[e], s[e + NS - NH]);
 #pragma unroll
                     for (int x = SPREAD; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
-                    const float m_new = fmaxf(m_run[e], fmaf(mx, q_scale, -kRefUnder));
+                    const float m_new = fmaxf(m_run[e], __fadd_rn(__fmul_rn(mx, q_scale), -kRefUnder));
                     alpha[e] = ex2(m_run[e] - m_new);
                     m_run[e] = m_new;
                     l_run[e] *= alpha[e];

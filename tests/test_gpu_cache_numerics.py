@@ -1,10 +1,10 @@
-"""Values that the cache's kernels must not lose: NaN and infinities in queries, keys, biases and gates."""
+"""Values that the cache's kernels must not lose: NaN and infinities in queries, keys, biases and gates; scores of any finite magnitude."""
 import numpy as np
 import pytest
 import torch
 
 from paper_2601_15305_b200 import binding as gsa
-from test_gpu_cache import BF16, GEOMETRIES, I32, _filled, _random_sets, f64, i32
+from test_gpu_cache import BF16, GEOMETRIES, I32, Pair, _filled, _random_sets, f64, i32
 
 pytestmark = pytest.mark.gpu
 NAN, INF = float("nan"), float("inf")
@@ -124,3 +124,41 @@ def test_a_nan_in_the_output_gate_shows(geo, sizes, k_max, Lq, G):
     assert torch.equal(out[kept], clean.cpu()[kept])
     want, mag = p.plain.attn(0, f64(Q[0, 0]), np.full((n_h, d), 60.0), np.asarray(sets[0][0]), d ** -0.5)
     assert abs(float(out[0, 0, 0, 1]) - want[0, 1]) <= 2.0 ** -8 * abs(want[0, 1]) + 2.0 ** -10 * mag[0, 1] and abs(float(out[0, 0, 0, 2])) <= 2.0 ** -100
+
+
+@pytest.mark.parametrize("exponent", [24, 27, 28, 29, 32, 40, 80, 110])
+@pytest.mark.parametrize("k_max", [40, 700])
+@pytest.mark.parametrize("geo", [GEOMETRIES[2], GEOMETRIES[4], GEOMETRIES[0]], ids=lambda g: "-".join(map(str, g.values())))
+@pytest.mark.parametrize("G", [1, 2, 4, 8])
+def test_scores_of_any_finite_magnitude(geo, G, k_max, exponent):
+    """Scores of 2^24 .. 2^110: far above the distance of neighbouring fp32 numbers there, the first key of a row takes it; keys that are alike share it."""
+    lens = [720, 730]
+    p = Pair(2, 2 * 740 // geo["T"] + 2, 740 // geo["T"] + 1, **geo, seed=80)
+    p.append([700, 710])
+    K, V, g2, kI = p.tokens(20, gate=False)
+    K[:, 10:] = K[:, :10]                                                # ten pairs of equal keys with values of their own
+    p.append([20, 20], x=(K, V, g2, kI))
+    sets = _random_sets(np.random.default_rng(G), [700, 710], 1, [k_max - 20, k_max - 21])
+    sets = [[np.concatenate([s[0], np.arange(n - 20, n)])] for s, n in zip(sets, lens)]
+    n_h, d = geo["n_kv"] * G, geo["d_h"]
+    gen = torch.Generator().manual_seed(81)
+    Q = (torch.randn(2, 1, n_h, d, generator=gen) * 2.0 ** exponent).to(BF16)
+    Q[0, 0, 0] = K[0, 4, 0] * 2.0 ** exponent                            # (one head's largest score is a pair's)
+    g1 = torch.randn(2, 1, n_h, d, generator=gen).to(BF16)
+    out = f64(_attention(p, G, 1, sets, k_max, Q, g1))
+    assert np.isfinite(out).all()
+    for b in range(2):
+        K64, V64, _ = p.plain.tokens(b, sets[b][0])
+        gate = 1 / (1 + np.exp(-f64(g1[b, 0])))
+        for h in range(n_h):
+            z = K64[:, h // G] @ f64(Q[b, 0, h]) * d ** -0.5
+            top = np.flatnonzero(z == z.max())
+            rest = np.delete(z, top)
+            # (scores are within 2^-14 of sum s |q|, below 2^-10 of the largest here; at a distance of 64 and more a key's part is below 2^-90)
+            if rest.max() > z.max() * (1 - 2.0 ** -9) - 64:
+                continue
+            want = V64[top, h // G].mean(0) * gate[h]
+            mag = np.abs(V64[top, h // G]).mean(0) * gate[h]
+            assert (np.abs(out[b, 0, h] - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -18 + 2.0 ** -11) * mag + 1e-25).all(), (b, h)
+            if (b, h) == (0, 0):
+                assert len(top) == 2
