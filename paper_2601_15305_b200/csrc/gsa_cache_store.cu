@@ -234,7 +234,7 @@ __device__ __forceinline__ void each_key_piece(const StoreArgs& a, const Token& 
 
 // What the first CTA of an append has to keep in the head: the status of a reservation that was refused, if tokens were given that it left
 // without a place.  (The mark alone does not tell: the caller may have made places of its own since, or given nothing.)
-__device__ __noinline__ int32_t refused_status(const StoreArgs& a) {
+__device__ __forceinline__ int32_t refused_status(const StoreArgs& a) {
     const int32_t status = a.ws[0];
     bool lost = false;
     for (int b = threadIdx.x; b < a.c.B; b += kStoreThreads) lost |= __ldg(a.start + b) < 0 && __ldg(a.n_new + b) > 0;
