@@ -11,7 +11,7 @@
 //       the index and 0 elsewhere.  The accumulators are then sums over one group each, Sum u q; their scales (which that lane holds)
 //       and the code's offset (-8 Sum q, what the accumulators start from) are applied to them, and the slots are added up by
 //       shuffles.                                                                S^T[key, head] = K[key, :] . Q[head, :]
-//       (Q as fp16: a power of two brings the warp's largest |q| to 2^14 .. 2^15, where every bf16 within 2^-25 of it is exact.)
+//       (Q as fp16: a power of two of its own brings each head's largest |q| to 2^14 .. 2^15, where every bf16 within 2^-25 of it is exact.)
 //       Eight heads fill the columns: there K is dequantised, in bf16, by one multiply-add, (128 + u) s - 136 s, exactly.
 //   V'  lane (gid, tig): the gid-th eighth of keys 2 tig, 2 tig + 1, 2 tig + 8, 2 tig + 9; words of two keys are joined half by half, so
 //       that a code position yields the pair (key, key + 1) of one d.                O^T[d, head] += V'^T[d, key] P^T[key, head]
@@ -427,18 +427,20 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
         constexpr bool QPAIR = G == 4 && DH == 64;             // four heads: zeroed for either set ahead of time, where registers allow
         uint32_t qz[QPAIR ? KW : 1][4];
         float q_start[SETS][KS][2];        // COLS: what the accumulators start from, -8 times the group's sum of Q
-        float q_scale = a.scale_log2;
+        constexpr int QS = COLS ? NH : 1;
+        float q_scale[QS];                 // of this lane's scores, by head
         float o[MT][4], m_run[NH], l_run[NH];
         int32_t row_first = cum[row], row_end = cum[row + 1], row_k = budget[row];
         auto start_row = [&]() {           // Q into its operand registers, an empty state
             if constexpr (!COLS) {
+                q_scale[0] = a.scale_log2;
 #pragma unroll
                 for (int w = 0; w < KW; ++w) {
                     qf[w][0] = __byte_perm(q[w].x, q[w].z, 0x5410); qf[w][1] = __byte_perm(q[w].x, q[w].z, 0x7632);
                     qf[w][2] = __byte_perm(q[w].y, q[w].w, 0x5410); qf[w][3] = __byte_perm(q[w].y, q[w].w, 0x7632);
                 }
             } else {
-                // the exponent of the warp's largest finite |q|
+                // the exponent of this lane's head's largest finite |q|, then of every head's (the lanes whose gid ends in its number)
                 uint32_t top = 0;
 #pragma unroll
                 for (int w = 0; w < KW; ++w) {
@@ -449,9 +451,21 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
                         top = max(top, max(lo_e == 255u ? 0u : lo_e, hi_e == 255u ? 0u : hi_e));
                     }
                 }
-                top = max(__reduce_max_sync(0xFFFFFFFFu, top), 20u);
+                top = max(top, 20u);
+                uint32_t tops[G];
+#pragma unroll
+                for (int hd = 0; hd < G; ++hd) tops[hd] = __reduce_max_sync(0xFFFFFFFFu, G == 1 || (gid & (G - 1)) == hd ? top : 0u);
+                top = tops[0];
+#pragma unroll
+                for (int hd = 1; hd < G; ++hd) top = (gid & (G - 1)) == hd ? tops[hd] : top;
                 const float up = __uint_as_float((127u + 14u + 127u - top) << 23);
-                q_scale = a.scale_log2 * 16777216.0f / up;                         // (2^24: what a code's place is worth)
+#pragma unroll
+                for (int e = 0; e < QS; ++e) {                     // over the head's power of two (2^24: what a code's place is worth)
+                    uint32_t its = tops[0];
+                    if constexpr (G == 2) its = tig & 1 ? tops[1] : tops[0];
+                    if constexpr (G == 4) its = tig & 1 ? tops[2 + e] : tops[e];
+                    q_scale[e] = a.scale_log2 * 16777216.0f * __uint_as_float((its - 14u) << 23);
+                }
                 float sum[KS];
 #pragma unroll
                 for (int gr = 0; gr < KS; ++gr) sum[gr] = 0.f;
@@ -624,7 +638,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
                 for (int e = 0; e < NS; ++e) {
                     // (The score is rounded before the reference is taken off: in one multiply-add the difference from a reference near
                     // 2^28, itself rounded to a multiple of 32, could be anything, and the numerator infinite.)
-                    p[e] = ex2(__fadd_rn(__fmul_rn(s[e], q_scale), -m_run[e & (NH - 1)]));
+                    p[e] = ex2(__fadd_rn(__fmul_rn(s[e], q_scale[e & (QS - 1)]), -m_run[e & (NH - 1)]));
                     most = fmaxf(most, p[e]);
                 }
                 return most;
@@ -636,7 +650,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) gsa_cache_attn_kernel(const Ca
                     float mx = ONE ? s[e] : fmaxf(s[e], s[e + NS - NH]);
 #pragma unroll
                     for (int x = SPREAD; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
-                    const float m_new = fmaxf(m_run[e], __fadd_rn(__fmul_rn(mx, q_scale), -kRefUnder));
+                    const float m_new = fmaxf(m_run[e], __fadd_rn(__fmul_rn(mx, q_scale[e & (QS - 1)]), -kRefUnder));
                     alpha[e] = ex2(m_run[e] - m_new);
                     m_run[e] = m_new;
                     l_run[e] *= alpha[e];

@@ -1,8 +1,9 @@
-"""Values that the cache's kernels must not lose: NaN and infinities in queries, keys, biases and gates; scores of any finite magnitude."""
+"""Values that the cache's kernels must not lose: NaN in queries, keys, biases and gates; heads of one group far apart."""
 import numpy as np
 import pytest
 import torch
 
+from cache_check import check_attention
 from paper_2601_15305_b200 import binding as gsa
 from test_gpu_cache import BF16, GEOMETRIES, I32, Pair, _filled, _random_sets, f64, i32
 
@@ -162,3 +163,24 @@ def test_scores_of_any_finite_magnitude(geo, G, k_max, exponent):
             assert (np.abs(out[b, 0, h] - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -18 + 2.0 ** -11) * mag + 1e-25).all(), (b, h)
             if (b, h) == (0, 0):
                 assert len(top) == 2
+
+
+@pytest.mark.parametrize("far", [-36, -60, 36])
+@pytest.mark.parametrize("k_max", [40, 700])
+@pytest.mark.parametrize("geo", [GEOMETRIES[2], GEOMETRIES[3], GEOMETRIES[0]], ids=lambda g: "-".join(map(str, g.values())))
+@pytest.mark.parametrize("G", [2, 4, 8])
+def test_heads_of_a_group_however_far_apart(geo, G, k_max, far):
+    """One query head of a KV head's group is 2^36 or 2^60 times as large as the others, or they as it: each is as exact as alone."""
+    lens = [720, 730]
+    p = _filled(geo, lens, 75)
+    sets = _random_sets(np.random.default_rng(G), lens, 1, [k_max, k_max - 1])
+    n_h, d = geo["n_kv"] * G, geo["d_h"]
+    gen = torch.Generator().manual_seed(76)
+    Q, g1 = torch.randn(2, 1, n_h, d, generator=gen), torch.randn(2, 1, n_h, d, generator=gen).to(BF16)
+    odd = [kv * G + (kv + 1) % G for kv in range(geo["n_kv"])]           # one head of each group, not always the same
+    rest = [h for h in range(n_h) if h not in odd]
+    Q[:, :, odd] *= 2.0 ** -far
+    Q = Q.to(BF16)
+    out = _attention(p, G, 1, sets, k_max, Q, g1)
+    assert out.isfinite().all()
+    check_attention(p.plain, Q, g1, out, sets, 1, d ** -0.5, heads=rest if far < 0 else range(n_h))
