@@ -463,10 +463,15 @@ int gsa_cache_compact(const gsa_cache_t *c, int32_t *live_pages, void *ws, size_
  * gsa_cache_topk: gsa_adaptive_topk for those rows.  A row that sees no key gets kt = 0 and var = 0.
  * gsa_cache_attn_fwd: gsa_sparse_gated_attn_fwd with K and V' from the cache.  Q, g1_logits, out [B, Lq, n_h, d_h] bf16,
  *   idx [B, Lq, k_max], kt [B, Lq]; the entries of a set may stand in any order.  A row with kt = 0 is written as zeros.
- *   Sums and softmax statistics are fp32.  For the product with V' the softmax numerators are rounded to fp16, scaled so that a row's
- *   largest lies between 2^7 and 2^15: to 2^-11 of one, or 2^-32 of the row's sum where that is more (2^-25 where scores exceed 2^24).  With up to four query heads a KV
- *   head a finite |q| sm_scale of 2^117 and more may count as infinite.  An infinity or NaN in Q, or in a selected K, makes the head's
- *   row NaN, one in a selected V' the 16 values that share its scale, a NaN in g1_logits its output.
+ *   Sums and softmax statistics are fp32.
+ *     scores       Up to four query heads a KV head: the 16 products that share a scale s are summed up from codes u, sum u q from -8 sum q on, to
+ *                  2^-14 s sum |q| however small the sum itself is (one channel far wider than its 15 neighbours costs them that much).
+ *                  q counts to 2^-35 of its head's largest; a finite |q| sm_scale of 2^117 and more may count as infinite.
+ *                  Eight heads: products of K and Q themselves.
+ *     numerators   For the product with V' they are rounded to fp16, scaled so that a row's largest lies between 2^7 and 2^15: to 2^-11 of one,
+ *                  or 2^-32 of the row's sum where that is more (2^-25 where scores exceed 2^24).
+ *   An infinity or NaN in Q, or in a selected K, makes the head's row NaN, one in a selected V' the 16 values that share its scale, a NaN
+ *   in g1_logits its output.
  *   ws: gsa_cache_attn_workspace_bytes(p).  The result does not depend on scheduling.
  */
 int gsa_cache_indexer_scores(const gsa_cache_t *c, const gsa_params_t *p, const void *qI, const float *w, const float *bI,

@@ -1,9 +1,9 @@
-"""Values that the cache's kernels must not lose: NaN in queries, keys, biases and gates; heads of one group far apart."""
+"""Values that the cache's kernels must not lose: NaN in queries, keys, biases and gates; heads of one group far apart; keys with outliers."""
 import numpy as np
 import pytest
 import torch
 
-from cache_check import check_attention
+from cache_check import check_attention, score_error
 from paper_2601_15305_b200 import binding as gsa
 from test_gpu_cache import BF16, GEOMETRIES, I32, Pair, _filled, _random_sets, f64, i32
 
@@ -184,3 +184,23 @@ def test_heads_of_a_group_however_far_apart(geo, G, k_max, far):
     out = _attention(p, G, 1, sets, k_max, Q, g1)
     assert out.isfinite().all()
     check_attention(p.plain, Q, g1, out, sets, 1, d ** -0.5, heads=rest if far < 0 else range(n_h))
+
+
+@pytest.mark.parametrize("G", [1, 2, 4, 8])
+@pytest.mark.parametrize("geo", [GEOMETRIES[0], GEOMETRIES[1], GEOMETRIES[4], GEOMETRIES[5]], ids=lambda g: "-".join(map(str, g.values())))
+def test_outliers_that_the_queries_do_not_look_at(geo, G):
+    """Every group of 16 has a channel 64 times as wide as the others, where Q is 0: scores far smaller than what they are summed up from."""
+    d, n = geo["d_h"], 400
+    p = Pair(1, n // geo["T"] + 2, n // geo["T"] + 1, **geo, seed=77)
+    gen = torch.Generator().manual_seed(78)
+    K, V = (torch.randn(1, n, geo["n_kv"], d, generator=gen) for _ in range(2))
+    K[..., 7::16] = 64 * K[..., 7::16].sign()
+    p.append([n], x=(K.to(BF16), V.to(BF16), None, torch.zeros(1, n, geo["dI"], dtype=BF16)))
+    Q = torch.randn(1, 1, geo["n_kv"] * G, d, generator=gen) * 4
+    Q[..., 7::16] = 0
+    Q, g1 = Q.to(BF16), torch.randn(1, 1, geo["n_kv"] * G, d, generator=gen).to(BF16)
+    sets = [[np.arange(n)]]
+    err, _ = score_error(p.plain, 0, f64(Q[0, 0]), sets[0][0], d ** -0.5)
+    assert err.max() < 0.05                                              # (the check below still tells something)
+    out = _attention(p, G, 1, sets, n, Q, g1)
+    check_attention(p.plain, Q, g1, out, sets, 1, d ** -0.5)
