@@ -351,6 +351,10 @@ def _extension():
             from . import _gsa_call as ext
         except ImportError as e:
             raise GsaError(f"{e}: build it with `python -m paper_2601_15305_b200.build`") from e
+        from .build import built_for
+        if getattr(ext, "built_for", None) != built_for():      # (nothing of it has run yet but its loading)
+            raise GsaError(f"the extension was built for {getattr(ext, 'built_for', 'something else')}, this is {built_for()}: "
+                           "build it again with `python -m paper_2601_15305_b200.build --force`")
         ext.bind(GsaError, *[at("gsa_cache_" + n) for n in _CALLS])
         _call, _ext = ext.call, ext
     return _ext

@@ -267,4 +267,12 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_gsa_call", nullptr, -1, methods, 
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__gsa_call(void) { return PyModule_Create(&module); }
+// (GSA_BUILT_FOR: the PyTorch and interpreter whose headers this was compiled with, which the binding compares with those that run)
+PyMODINIT_FUNC PyInit__gsa_call(void) {
+    PyObject* m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "built_for", GSA_BUILT_FOR) < 0) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}
