@@ -359,7 +359,8 @@ int gsa_forward_host(const gsa_params_t *p, const void *Q, const void *K, const 
  * A pool of n_pages pages of page_tokens tokens each.  table[b, s / page_tokens] is the page that holds position s of sequence
  * b; lens[b] is the number of its tokens; refs[page] says how many table entries name the page (0: free).  Several sequences
  * may name one page; only a sequence's last page can be partly filled, and that one is never shared.  An empty cache has
- * table = -1, lens = 0, refs = 0 and any bytes in its pool.  All four arrays are the caller's device memory; the calls below
+ * table = -1, lens = 0, refs = 0 and any bytes in its pool.  One row of the table and its length, with the same pool and refs and
+ * B = 1, are a cache too: that sequence alone, for its prompt (gsa_cache_compact takes the whole table).  All four arrays are the caller's device memory; the calls below
  * change them on the device, in stream order, without waiting for the host, and can be captured into a graph.
  *
  * A token's record: D / 2 bytes of K codes, D / 2 bytes of V' codes, D / 8 scale bytes (D = n_kv * d_h), padded to a

@@ -19,7 +19,7 @@
 //       times s: every value of the format is exact in fp16 too (105 * 2^-23 .. 7 * 3584).
 // The tile's numerators are rounded to fp16 for the second product.  They are taken against a reference that leaves a row's largest
 // between 2^7 and 2^15, so that rounding is at most 2^-11 of a numerator, or 2^-25 where that is less than fp16's normal range goes down
-// to: 2^-32 of the row's sum.  (In bf16, 2^-8 of each, the error of the 32 x 128K case against 64 bits is 2.3e-3; with fp16 it is
+// to: 2^-32 of the row's sum.  (Scores above 2^24, whose neighbours in fp32 lie 2 and more apart, leave a row's largest at 2^0 to 2^14.  In bf16, 2^-8 of each, the error of the 32 x 128K case against 64 bits is 2.3e-3; with fp16 it is
 // 1.7e-3, the output's own rounding.)  Statistics, scores and sums are fp32.
 //
 // Records come by asynchronous copies into a ring of kStages tiles a warp (2560 bytes each at d_h = 128, V' rows padded), so that some 70 to
@@ -35,9 +35,9 @@
 //
 // Bound: the issue of instructions, some 500 for a tile and KV head, by four warps a scheduler (the registers allow no more; 57 % of all
 // cycles issue one, and most others wait for a fixed latency or the ALU).  32 sequences of 16K to 128K, 16 heads on 8 KV heads of 128: 71 MB of
-// records, 30.0 us with the merge, 2.4 TB/s; some 6 us pass before the first tile (budgets, indices, pages, records: four loads in a
-// row), 18 us in the loop, 6 us from its end to the end of the merge.  257 rows of 1000 of 20011 keys, 32 heads on 8 of 64: 60 us.
-// (Four query heads at d_h = 128 spill 88 to 220 bytes a thread.)
+// records, 30.0 us with the merge (29.4 with one power of two for a KV head's queries instead of one a head; chunk 58.9), 2.4 TB/s; some 6 us pass before the first tile (budgets, indices, pages, records: four loads in a
+// row), 18 us in the loop, 6 us from its end to the end of the merge.  257 rows of 1000 of 20011 keys, 32 heads on 8 of 64: 60.6 us.
+// (Four query heads at d_h = 128 spill 108 to 244 bytes a thread: 16 sequences of 4K to 32K, 8 KV heads, 26.4 us, with two heads 21.7.)
 #include "gsa_cache.cuh"
 
 #include <cuda_fp16.h>

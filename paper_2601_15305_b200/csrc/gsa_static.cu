@@ -43,7 +43,6 @@ cudaError_t scratch_on_current_device(void** ptr) {
     return cudaSuccess;
 }
 
-
 }  // namespace
 
 cudaError_t static_scratch_address(void** ptr) { return scratch_on_current_device(ptr); }
