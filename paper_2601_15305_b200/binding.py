@@ -338,7 +338,7 @@ _call = _ext = None
 
 
 def _address(name: str) -> int:
-    """Where the library's function is; loads the extension (built with the library) at the first use."""
+    """Where the library's function is, for _call, which takes any (tests; the calls below do not go by it); loads the extension at the first use."""
     _extension()
     return ctypes.cast(getattr(lib(), name), ctypes.c_void_p).value
 

@@ -4,7 +4,8 @@
 //
 // call(address, a, b, ...) calls any function of the library that takes up to sixteen integers or pointers and returns an int, with the
 // given ints (None: NULL).  In the x86-64 and AArch64 calling conventions a narrower integer argument occupies a whole register or stack
-// slot, so that all of them can be passed as 64 bits.
+// slot, so that all of them can be passed as 64 bits.  The binding's calls go by the functions further down, which check their arguments; this one
+// checks nothing and serves the test of the calling convention.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/core/Tensor.h>
