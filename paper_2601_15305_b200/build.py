@@ -90,7 +90,7 @@ def _build_library(verbose: bool) -> None:
         procs.append((cmd, _start(cmd)))
     for cmd, pr in procs:
         _finish(cmd, pr, verbose)
-    tmp = LIB_PATH + f".tmp{os.getpid()}"
+    tmp = os.path.join(objdir, f"library.{os.getpid()}.so")
     subprocess.check_call([NVCC, "-shared", "-o", tmp, *objs, "-lcudart", "-ldl"])
     os.replace(tmp, LIB_PATH)
 
@@ -100,11 +100,11 @@ def _build_call(verbose: bool) -> None:
     for old in (CALL_STAMP, CALL_PATH):
         if os.path.exists(old):
             os.remove(old)
-    tmp = CALL_PATH + f".tmp{os.getpid()}"
+    os.makedirs(os.path.dirname(CALL_STAMP), exist_ok=True)
+    tmp = os.path.join(os.path.dirname(CALL_STAMP), f"call.{os.getpid()}.so")
     cmd = _call_command(tmp)
     _finish(cmd, _start(cmd), verbose)
     os.replace(tmp, CALL_PATH)
-    os.makedirs(os.path.dirname(CALL_STAMP), exist_ok=True)
     with open(CALL_STAMP, "w") as f:
         f.write(built_for())
 

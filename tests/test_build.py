@@ -37,6 +37,17 @@ def test_the_library_stands_without_a_cpp_compiler(away, monkeypatch):
     assert not (away / "call.so").exists()
 
 
+def test_a_failure_leaves_nothing_beside_the_outputs(away, monkeypatch):
+    """Files of a compiler that fails after it has written stay among the objects, which no commit takes up."""
+    fake = away / "compiler"
+    fake.write_text('#!/bin/sh\nwhile [ "$1" != "-o" ]; do shift; done\ntouch "$2"\nexit 1\n')
+    fake.chmod(0o755)
+    monkeypatch.setattr(build, "CXX", str(fake))
+    with pytest.warns(RuntimeWarning):
+        build.build()
+    assert {p.name for p in away.iterdir()} == {"compiler", "lib.so", "objects"} and list((away / "objects").iterdir())
+
+
 def test_a_failing_library_is_an_error(away, monkeypatch):
     monkeypatch.setattr(build, "NVCC", "false")
     monkeypatch.setattr(build, "_PKG", str(away))
